@@ -469,6 +469,109 @@ int axonn_adam_bucket(uint64_t n, float* theta, float* m, float* v, const void* 
                       double weight_decay, int64_t step, double grad_scale, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------
+ * Operations of a training step around the layer's own: a scaled token embedding, norms of
+ * queries and keys with the position rotation, dropout, and linear maps in 8-bit floating
+ * point.  The conventions of the single operations above hold, and: matrices may start at any
+ * element and have any leading dimension (>= their width, in elements) unless a call says
+ * otherwise; sums are fp32 and in a fixed order, every result is rounded once; nothing is
+ * allocated and all calls may be captured into a graph; a result may overlap an operand only
+ * where that is stated, and then only exactly (same address, same leading dimension); the
+ * device that is current at the call is the one used.  Calls that may overlap each other need
+ * workspaces of their own.
+ * ---------------------------------------------------------------------------------- */
+
+/* out[t,:] = scale * table[tokens[t],:], t < T; table [vocab, h] dense, out [T, h] with ld_out.
+ * Ids outside [0, vocab) are clamped into range.  T <= 2^24, h <= 65535, vocab <= 2^30,
+ * vocab * h <= 2^34. */
+int axonn_embedding_fwd(int64_t T, int64_t h, int64_t vocab, const int32_t* tokens,
+                        const void* table_bf16, float scale, void* out_bf16, int64_t ld_out,
+                        void* hip_stream);
+/* Its gradient: dtable[v,:] = (accumulate ? dtable[v,:] : 0) + scale * sum of dout[t,:] over the
+ * tokens t of id v, in token order (ids are sorted on the device first).  Without accumulate
+ * every row of dtable is written (zeros for ids that do not occur), with it only the rows of ids
+ * that do.  dtable [vocab, h] dense, float32 if dtable_fp32, else 16-bit; the result has the same
+ * bits every time.  workspace: the number of bytes that _workspace returns, 16-byte aligned. */
+int axonn_embedding_bwd_workspace(int64_t T, int64_t h, int64_t vocab, uint64_t* bytes);
+int axonn_embedding_bwd(int64_t T, int64_t h, int64_t vocab, const int32_t* tokens,
+                        const void* dout_bf16, int64_t ld_dout, float scale, void* dtable,
+                        int32_t dtable_fp32, int32_t accumulate, void* workspace,
+                        void* hip_stream);
+
+/* Packed rows [Q | K | V] of n_heads, n_kv_heads and n_kv_heads heads (with n_kv_heads = n_heads
+ * the layout axonn_attention_fwd reads).  Every query and key head x of a token is normalised and
+ * rotated, V is copied:
+ *   z = gamma * x / sqrt(mean(x^2) + eps)              gamma_q, gamma_k: [head_dim] each
+ *   (z_a, z_b) -> (z_a cos - z_b sin, z_a sin + z_b cos),  angle = position * inv_freq[i]
+ * for the pairs i < rotary_dim / 2: (a, b) = (i, i + rotary_dim / 2), or (2i, 2i + 1) if
+ * interleaved; elements from rotary_dim on are not rotated.  The position of token t is
+ * positions[t] (device, any int32), or t % seq_len if positions is NULL.  inv_freq: device array
+ * of rotary_dim / 2 doubles (e.g. base^(-2i / rotary_dim); NULL allowed if rotary_dim is 0).
+ * head_dim even, at most 256; rotary_dim even, at most head_dim; eps > 0; T <= 2^24.
+ * out may be qkv (V is then left alone); columns of out behind the three parts are not written. */
+int axonn_qk_norm_rope_fwd(int64_t T, int32_t seq_len, int32_t n_heads, int32_t n_kv_heads,
+                           int32_t head_dim, int32_t rotary_dim, int32_t interleaved,
+                           const void* qkv_bf16, int64_t ld_qkv, const void* gamma_q_bf16,
+                           const void* gamma_k_bf16, float eps, const int32_t* positions,
+                           const double* inv_freq, void* out_bf16, int64_t ld_out,
+                           void* hip_stream);
+/* Its gradient.  dout: the gradient of `out` (as axonn_attention_bwd writes it); qkv: the forward
+ * call's input.  dqkv: the gradient of qkv (V's part is copied), may be dout or qkv.  dgamma_q,
+ * dgamma_k float32 [head_dim] are overwritten with the sums over tokens and heads.
+ * workspace: the number of bytes that _workspace returns, 16-byte aligned. */
+int axonn_qk_norm_rope_bwd_workspace(int64_t T, int32_t n_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, uint64_t* bytes);
+int axonn_qk_norm_rope_bwd(int64_t T, int32_t seq_len, int32_t n_heads, int32_t n_kv_heads,
+                           int32_t head_dim, int32_t rotary_dim, int32_t interleaved,
+                           const void* dout_bf16, int64_t ld_dout, const void* qkv_bf16,
+                           int64_t ld_qkv, const void* gamma_q_bf16, const void* gamma_k_bf16,
+                           float eps, const int32_t* positions, const double* inv_freq,
+                           void* dqkv_bf16, int64_t ld_dqkv, float* dgamma_q, float* dgamma_k,
+                           void* workspace, void* hip_stream);
+
+/* Dropout from a counter-based generator: out = (res ? res : 0) + keep * x / (1 - p).  Whether
+ * element (r, c) of x [T, h] is kept depends on (seed, offset, r, c) alone, so no mask is stored:
+ * the backward pass, and a forward pass that is run again, take the same seed and offset; calls
+ * that are to drop independently take different ones.  p in [0, 1] is rounded to a multiple of
+ * 2^-16, and kept elements are divided by the rounded probability of being kept.  Dropped
+ * elements are exact zeros, whatever x holds there; with p = 1 all are.
+ * The generator is Philox4x32-10 (Salmon et al. 2011): columns 8g .. 8g+7 of row r take the 16-bit
+ * halves, low first, of the four words for key (seed low, seed high) and counter (g, r, offset
+ * low, offset high); an element is kept if its half is >= round(65536 p).
+ * offset_dev: NULL, or one device uint64 that is added to offset when the kernel runs (a captured
+ * graph reads it anew at every replay).  out may be x or res.  T, h <= 2^24. */
+int axonn_dropout_fwd(int64_t T, int64_t h, const void* x_bf16, int64_t ld_x,
+                      const void* res_bf16, int64_t ld_res, float p, uint64_t seed,
+                      uint64_t offset, const uint64_t* offset_dev, void* out_bf16,
+                      int64_t ld_out, void* hip_stream);
+/* dx = keep * dout / (1 - p); the residual's gradient is dout itself.  dx may be dout. */
+int axonn_dropout_bwd(int64_t T, int64_t h, const void* dout_bf16, int64_t ld_dout, float p,
+                      uint64_t seed, uint64_t offset, const uint64_t* offset_dev,
+                      void* dx_bf16, int64_t ld_dx, void* hip_stream);
+
+/* 8-bit form of a matrix: e4m3 codes (the OCP format without infinities; largest value 448) with
+ * a scale for each block of 128 elements along the contraction.  The scale is the least power of
+ * two 2^e, e >= -127, with which the block's largest finite magnitude is at most 448 * 2^e, stored
+ * as the byte e + 127 (0 for a block of zeros); a code is x / 2^e rounded to nearest, ties to even.
+ * An infinity or NaN becomes the code of NaN and has no part in the scale.
+ * A form of a matrix with rows of K elements: codes [rows][Kp], Kp = 128 * ceil(K / 128), zeros
+ * behind K; scales [rows][4 * ceil(Kp / 512)], zeros behind the last block.
+ * x [R, C]: q, scale receive its rows (blocks along C), q_t, scale_t the rows of its transpose
+ * (C rows of R elements, blocks along R).  Either pair may be NULL; x is read once for both.
+ * Codes 16-byte aligned, scales 4-byte aligned.  R, C <= 2^22. */
+int axonn_fp8_quantize(int64_t R, int64_t C, const void* x_bf16, int64_t ld_x, void* q,
+                       uint8_t* scale, void* q_t, uint8_t* scale_t, void* hip_stream);
+/* C[M,N] = epilogue( sum_k A(m,k) * B(n,k) ) of two matrices in that form (M and N rows of K
+ * elements), fp32 accumulation; the epilogues are axonn_gemm_bf16's, each allowed for any operands.
+ * With x [T, in], W [in, out], dy [T, out]: the forward map takes the rows of x and of W's transpose
+ * (K = in), the input gradient the rows of dy and of W (K = out), the weight gradient the rows of
+ * x's and of dy's transpose (K = T).  M, N, K <= 2^22, M * N <= 2^38, otherwise any; C may be res or
+ * (epilogue 3) aux. */
+int axonn_gemm_fp8(int32_t epilogue, int64_t M, int64_t N, int64_t K, const void* A,
+                   const uint8_t* a_scale, const void* B, const uint8_t* b_scale, void* C,
+                   int64_t ldc, const void* bias, const void* res, int64_t ld_res, void* aux,
+                   int64_t ld_aux, int32_t accumulate, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------
  * Launch timing (measurement aid, off by default).  While enabled, every kernel launch the
  * library makes is bracketed by a pair of HIP events on the stream it is launched on;
  * collect() waits for them, adds up elapsed milliseconds and launch counts per category
@@ -477,7 +580,7 @@ int axonn_adam_bucket(uint64_t n, float* theta, float* m, float* v, const void* 
  * forms several weight gradients counts as that many), attention
  * forward / backward, LayerNorm forward / backward (the backward with the reduction of its
  * gain and shift gradients), gradient conversion, Adam, input copy, embedding,
- * cross-entropy.  Process-wide, not thread-safe.  Intervals of kernels that overlap on different streams are each counted
+ * cross-entropy, query / key norms with rotation, dropout, 8-bit quantiser, 8-bit products.  Process-wide, not thread-safe.  Intervals of kernels that overlap on different streams are each counted
  * in full.
  * ---------------------------------------------------------------------------------- */
 int axonn_profile_enable(int32_t on);

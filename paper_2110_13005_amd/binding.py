@@ -123,6 +123,17 @@ _PROTOTYPES = {
     "axonn_colsum": [_i64, _i64, _vp, _i64, _vp, _vp, _vp],
     "axonn_attention_fwd": [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp],
     "axonn_attention_bwd": [_i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
+    "axonn_embedding_fwd": [_i64, _i64, _i64, _vp, _vp, _f, _vp, _i64, _vp],
+    "axonn_embedding_bwd_workspace": [_i64, _i64, _i64, C.POINTER(_u64)],
+    "axonn_embedding_bwd": [_i64, _i64, _i64, _vp, _vp, _i64, _f, _vp, _i32, _i32, _vp, _vp],
+    "axonn_qk_norm_rope_fwd": [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _f, _vp, _vp, _vp, _i64, _vp],
+    "axonn_qk_norm_rope_bwd_workspace": [_i64, _i32, _i32, _i32, C.POINTER(_u64)],
+    "axonn_qk_norm_rope_bwd": [_i64, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _f, _vp, _vp, _vp, _i64,
+                               _vp, _vp, _vp, _vp],
+    "axonn_dropout_fwd": [_i64, _i64, _vp, _i64, _vp, _i64, _f, _u64, _u64, _vp, _vp, _i64, _vp],
+    "axonn_dropout_bwd": [_i64, _i64, _vp, _i64, _f, _u64, _u64, _vp, _vp, _i64, _vp],
+    "axonn_fp8_quantize": [_i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp],
+    "axonn_gemm_fp8": [_i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i32, _vp],
     "axonn_profile_enable": [_i32],
     "axonn_profile_num_categories": [C.POINTER(_i32)],
     "axonn_profile_category_name": [_i32, C.POINTER(C.c_char_p)],
@@ -499,6 +510,61 @@ def axonn_adam_bucket(n, theta, m, v, grad16, param16, lr, beta1, beta2, eps, we
                       stream=None):
     _call("axonn_adam_bucket", n, _ptr(theta), _ptr(m), _ptr(v), _ptr(grad16), _ptr(param16), lr, beta1, beta2,
                                     eps, weight_decay, step, grad_scale, _stream(stream))
+
+
+def axonn_embedding_fwd(T, h, vocab, tokens, table, scale, out, ld_out, stream=None):
+    _call("axonn_embedding_fwd", T, h, vocab, _ptr(tokens), _ptr(table), scale, _ptr(out), ld_out, _stream(stream))
+
+
+def axonn_embedding_bwd_workspace(T, h, vocab):
+    """Bytes of workspace that axonn_embedding_bwd needs."""
+    n = _u64()
+    _call("axonn_embedding_bwd_workspace", T, h, vocab, C.byref(n))
+    return n.value
+
+
+def axonn_embedding_bwd(T, h, vocab, tokens, dout, ld_dout, scale, dtable, dtable_fp32, accumulate, workspace, stream=None):
+    _call("axonn_embedding_bwd", T, h, vocab, _ptr(tokens), _ptr(dout), ld_dout, scale, _ptr(dtable), dtable_fp32, accumulate,
+          _ptr(workspace), _stream(stream))
+
+
+def axonn_qk_norm_rope_fwd(T, seq_len, n_heads, n_kv_heads, head_dim, rotary_dim, interleaved, qkv, ld_qkv, gamma_q, gamma_k, eps,
+                           positions, inv_freq, out, ld_out, stream=None):
+    _call("axonn_qk_norm_rope_fwd", T, seq_len, n_heads, n_kv_heads, head_dim, rotary_dim, interleaved, _ptr(qkv), ld_qkv,
+          _ptr(gamma_q), _ptr(gamma_k), eps, _ptr(positions), _ptr(inv_freq), _ptr(out), ld_out, _stream(stream))
+
+
+def axonn_qk_norm_rope_bwd_workspace(T, n_heads, n_kv_heads, head_dim):
+    """Bytes of workspace that axonn_qk_norm_rope_bwd needs."""
+    n = _u64()
+    _call("axonn_qk_norm_rope_bwd_workspace", T, n_heads, n_kv_heads, head_dim, C.byref(n))
+    return n.value
+
+
+def axonn_qk_norm_rope_bwd(T, seq_len, n_heads, n_kv_heads, head_dim, rotary_dim, interleaved, dout, ld_dout, qkv, ld_qkv, gamma_q,
+                           gamma_k, eps, positions, inv_freq, dqkv, ld_dqkv, dgamma_q, dgamma_k, workspace, stream=None):
+    _call("axonn_qk_norm_rope_bwd", T, seq_len, n_heads, n_kv_heads, head_dim, rotary_dim, interleaved, _ptr(dout), ld_dout, _ptr(qkv),
+          ld_qkv, _ptr(gamma_q), _ptr(gamma_k), eps, _ptr(positions), _ptr(inv_freq), _ptr(dqkv), ld_dqkv, _ptr(dgamma_q),
+          _ptr(dgamma_k), _ptr(workspace), _stream(stream))
+
+
+def axonn_dropout_fwd(T, h, x, ld_x, res, ld_res, p, seed, offset, offset_dev, out, ld_out, stream=None):
+    _call("axonn_dropout_fwd", T, h, _ptr(x), ld_x, _ptr(res), ld_res, p, seed, offset, _ptr(offset_dev), _ptr(out), ld_out,
+          _stream(stream))
+
+
+def axonn_dropout_bwd(T, h, dout, ld_dout, p, seed, offset, offset_dev, dx, ld_dx, stream=None):
+    _call("axonn_dropout_bwd", T, h, _ptr(dout), ld_dout, p, seed, offset, _ptr(offset_dev), _ptr(dx), ld_dx, _stream(stream))
+
+
+def axonn_fp8_quantize(R, C_, x, ld_x, q=None, scale=None, q_t=None, scale_t=None, stream=None):
+    _call("axonn_fp8_quantize", R, C_, _ptr(x), ld_x, _ptr(q), _ptr(scale), _ptr(q_t), _ptr(scale_t), _stream(stream))
+
+
+def axonn_gemm_fp8(epilogue, M, N, K, A, a_scale, B, b_scale, Cmat, ldc, bias=None, res=None, ld_res=0, aux=None, ld_aux=0,
+                   accumulate=0, stream=None):
+    _call("axonn_gemm_fp8", epilogue, M, N, K, _ptr(A), _ptr(a_scale), _ptr(B), _ptr(b_scale), _ptr(Cmat), ldc, _ptr(bias), _ptr(res),
+          ld_res, _ptr(aux), ld_aux, accumulate, _stream(stream))
 
 
 TUNE_GEMM_COPY_MASK, TUNE_GEMM_BIG_MIN_TILES, TUNE_GEMM_TILE_N = 0, 1, 2

@@ -126,6 +126,13 @@ __device__ __forceinline__ void dma_chunk16(u32x4 rsrc, uint32_t voffset, uint32
                : "s"(lds_addr), "v"(voffset), "s"(rsrc), "s"(soffset)
                : "memory");
 }
+// The same for 64 words of 4 bytes.
+__device__ __forceinline__ void dma_word(u32x4 rsrc, uint32_t voffset, uint32_t soffset, uint32_t lds_addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+               :
+               : "s"(lds_addr), "v"(voffset), "s"(rsrc), "s"(soffset)
+               : "memory");
+}
 __device__ __forceinline__ void dma_wait_all() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 // Buffer descriptor words of `bytes` bytes at p (raw buffer, offsets at or beyond `bytes` read zeros).
 __device__ __forceinline__ u32x4 rsrc_words(const void* p, uint32_t bytes) {
@@ -338,6 +345,26 @@ hipError_t launch_embed_bwd(int b, int s, int h, int vocab, const int* tokens, c
 // the logits are overwritten by dloss/dlogits.
 hipError_t launch_xent(int T, int V, void* logits, const int* targets, int n_microbatches, float loss_scale,
                        float* token_loss, float* loss, hipStream_t st);
+// Operators of embedding.hip, qk_norm.hip, dropout.hip and fp8.hip.  threshold: dropped 65536ths.
+hipError_t launch_embedding_fwd(int64_t T, int64_t h, int64_t vocab, const int* tokens, const void* table, float scale, void* out,
+                                int64_t ld_out, hipStream_t s);
+uint64_t embedding_bwd_ws_bytes(int64_t T, int64_t h, int64_t vocab);
+hipError_t launch_embedding_bwd(int64_t T, int64_t h, int64_t vocab, const int* tokens, const void* dout, int64_t ld_dout, float scale,
+                                void* dtable, bool fp32, bool accumulate, void* workspace, hipStream_t s);
+struct QkShape { int64_t T; int seq, heads, kv, d, rot; bool interleaved; };
+hipError_t launch_qk_norm_rope_fwd(const QkShape& q, const void* qkv, int64_t ld_qkv, const void* gamma_q, const void* gamma_k, float eps,
+                                   const int* positions, const double* inv_freq, void* out, int64_t ld_out, hipStream_t s);
+uint64_t qk_norm_rope_bwd_ws_bytes(int64_t T, int d);
+hipError_t launch_qk_norm_rope_bwd(const QkShape& q, const void* dout, int64_t ld_dout, const void* qkv, int64_t ld_qkv, const void* gamma_q,
+                                   const void* gamma_k, float eps, const int* positions, const double* inv_freq, void* dqkv,
+                                   int64_t ld_dqkv, float* dgamma_q, float* dgamma_k, float* workspace, hipStream_t s);
+hipError_t launch_dropout(int64_t T, int64_t h, const void* x, int64_t ld_x, const void* res, int64_t ld_res, uint32_t threshold,
+                          uint64_t seed, uint64_t offset, const uint64_t* offset_dev, void* out, int64_t ld_out, hipStream_t s);
+hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x, void* q, void* scale, void* q_t, void* scale_t,
+                               hipStream_t s);
+hipError_t launch_gemm_fp8(int epi, int64_t M, int64_t N, int64_t K, const void* A, const void* a_scale, const void* B, const void* b_scale,
+                           void* C, int64_t ldc, const void* bias, const void* res, int64_t ld_res, void* aux, int64_t ld_aux,
+                           int accumulate, hipStream_t s);
 hipError_t launch_adam(uint64_t n, float* theta, float* m, float* v, const void* g16,
                        void* p16, double lr, double b1, double b2, double eps, double wd,
                        int64_t step, double grad_scale, hipStream_t s);

@@ -1,0 +1,405 @@
+// Linear maps in 8-bit floating point (e4m3: 4 bits of exponent, 3 of significand, largest 448) with a scale for each block of
+// 128 elements along the contraction.
+//
+// The scale is a power of two, 2^e with the least e for which the block's largest magnitude is at most 448 * 2^e, stored as the
+// byte e + 127: the form in which gfx950's scaled MFMA takes it as an operand, so the product's loop has no vector
+// instruction for it.  x * 2^-e is exact, so a code is one rounding of x (to nearest, ties to even), however it is formed.
+//
+// Quantised matrices: codes [rows][Kp], Kp = K rounded up to 128, zeros behind K; scales [rows][S], S = Kp / 128 rounded up to
+// 4: a row's scales of four blocks are one 32-bit word, of which the MFMA picks a byte by an immediate.
+#include "rows.h"
+#include "host_logic.h"
+#include <algorithm>
+
+namespace axonn {
+
+constexpr int FB = 128;                      // elements of a block
+
+// ---------------------------------------------------------------------------------------------------------- quantiser
+// e of a block from its largest finite magnitude.
+__device__ __forceinline__ int block_exponent(float amax) {
+  const uint32_t b = __float_as_uint(amax);
+  return max(-127, (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0));       // 448 = 1.75 * 2^8
+}
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
+__device__ __forceinline__ float finite_magnitude(float v) {
+  const float a = fabsf(v);
+  return a < INFINITY ? a : 0.f;             // an infinity or NaN has no part in the scale
+}
+// Codes of four values, the first in the low byte; an infinity or NaN becomes the code of NaN.
+__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float inv) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+  uint32_t bad = 0;
+  if (!(fabsf(a) < INFINITY)) bad |= 0x7fu;
+  if (!(fabsf(b) < INFINITY)) bad |= 0x7f00u;
+  if (!(fabsf(c) < INFINITY)) bad |= 0x7f0000u;
+  if (!(fabsf(d) < INFINITY)) bad |= 0x7f000000u;
+  return (uint32_t)w | bad;
+}
+
+struct QuantArgs {
+  int R, C;                 // rows and columns of x
+  const elem_t* x;
+  int64_t ld_x;
+  uint8_t *q, *scale;       // [R][Cp], [R][S]         (null: not wanted)
+  uint8_t *q_t, *scale_t;   // [C][Rp], [C][S_t]
+  int64_t Cp, S, Rp, S_t;
+};
+
+// One workgroup per block of 128 x 128 elements.  Read once; the rows' codes come straight from the registers, the columns'
+// through LDS: a thread owns two adjacent columns of a quarter of the rows.
+// Scale bytes behind the last block are cleared by the workgroup of that block.
+constexpr int QT_LD = FB + 8;                // elements of an LDS row
+template <bool ROWS, bool COLS>
+__global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantArgs g) {
+  __shared__ __align__(16) elem_t tile[COLS ? FB * QT_LD : 8];
+  __shared__ float col_max[COLS ? 4 : 1][FB];
+  __shared__ __align__(16) uint8_t codes_t[COLS ? FB * FB : 16];
+  const int tid = threadIdx.x, c0 = blockIdx.x * FB, r0 = blockIdx.y * FB;
+  const int ch = tid & 15, n = g.C - (c0 + 8 * ch);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int r = i * 16 + (tid >> 4), row = r0 + r;
+    elemx8 v = {};
+    if (row < g.R && n > 0) v = load_chunk(g.x + (int64_t)row * g.ld_x + c0 + 8 * ch, n);
+    if (COLS) *reinterpret_cast<elemx8*>(tile + r * QT_LD + 8 * ch) = v;
+    if (ROWS) {
+      float f[8], amax = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        f[e] = (float)v[e];
+        amax = fmaxf(amax, finite_magnitude(f[e]));
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
+      const int ex = block_exponent(amax);
+      const float inv = exp2_int(-ex);
+      if (row < g.R) {
+        *reinterpret_cast<u32x2*>(g.q + (int64_t)row * g.Cp + c0 + 8 * ch) =
+            u32x2{encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv)};
+        const int last = (int)(g.Cp / FB) - 1, at = blockIdx.x;
+        if (ch == 0) g.scale[(int64_t)row * g.S + at] = (uint8_t)(ex + 127);
+        else if (at == last && at + ch < g.S) g.scale[(int64_t)row * g.S + at + ch] = 0;
+      }
+    }
+  }
+  if (!COLS) return;
+  __syncthreads();
+  const int pair = tid & 63, quarter = tid >> 6;
+  float m0 = 0.f, m1 = 0.f;
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+    const elemx2 v = *reinterpret_cast<const elemx2*>(tile + (quarter * 32 + r) * QT_LD + 2 * pair);
+    m0 = fmaxf(m0, finite_magnitude((float)v[0]));
+    m1 = fmaxf(m1, finite_magnitude((float)v[1]));
+  }
+  col_max[quarter][2 * pair] = m0;
+  col_max[quarter][2 * pair + 1] = m1;
+  __syncthreads();
+  m0 = fmaxf(fmaxf(col_max[0][2 * pair], col_max[1][2 * pair]), fmaxf(col_max[2][2 * pair], col_max[3][2 * pair]));
+  m1 = fmaxf(fmaxf(col_max[0][2 * pair + 1], col_max[1][2 * pair + 1]), fmaxf(col_max[2][2 * pair + 1], col_max[3][2 * pair + 1]));
+  const int e0 = block_exponent(m0), e1 = block_exponent(m1);
+  const float i0 = exp2_int(-e0), i1 = exp2_int(-e1);
+#pragma unroll
+  for (int r = 0; r < 32; r += 4) {
+    elemx2 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const elemx2*>(tile + (quarter * 32 + r + k) * QT_LD + 2 * pair);
+    *reinterpret_cast<uint32_t*>(codes_t + (2 * pair) * FB + quarter * 32 + r) =
+        encode4((float)v[0][0], (float)v[1][0], (float)v[2][0], (float)v[3][0], i0);
+    *reinterpret_cast<uint32_t*>(codes_t + (2 * pair + 1) * FB + quarter * 32 + r) =
+        encode4((float)v[0][1], (float)v[1][1], (float)v[2][1], (float)v[3][1], i1);
+  }
+  const int last = (int)(g.Rp / FB) - 1, at = blockIdx.y;
+  if (quarter == 0) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int col = c0 + 2 * pair + k;
+      if (col >= g.C) continue;
+      g.scale_t[(int64_t)col * g.S_t + at] = (uint8_t)((k ? e1 : e0) + 127);
+      if (at == last)
+        for (int b = at + 1; b < g.S_t; ++b) g.scale_t[(int64_t)col * g.S_t + b] = 0;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = i * 32 + (tid >> 3);
+    if (c0 + col < g.C)
+      *reinterpret_cast<u32x4*>(g.q_t + (int64_t)(c0 + col) * g.Rp + r0 + 16 * (tid & 7)) =
+          *reinterpret_cast<const u32x4*>(codes_t + col * FB + 16 * (tid & 7));
+  }
+}
+
+hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x, void* q, void* scale, void* q_t, void* scale_t,
+                               hipStream_t s) {
+  QuantArgs g;
+  g.R = (int)R; g.C = (int)C; g.x = (const elem_t*)x; g.ld_x = ld_x;
+  g.q = (uint8_t*)q; g.scale = (uint8_t*)scale; g.q_t = (uint8_t*)q_t; g.scale_t = (uint8_t*)scale_t;
+  g.Cp = (C + FB - 1) / FB * FB; g.Rp = (R + FB - 1) / FB * FB;
+  g.S = (g.Cp / FB + 3) / 4 * 4; g.S_t = (g.Rp / FB + 3) / 4 * 4;
+  const dim3 grid((unsigned)(g.Cp / FB), (unsigned)(g.Rp / FB));
+  if (q && q_t) hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_kernel<true, true>), grid, dim3(256), 0, s, g);
+  else if (q) hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_kernel<true, false>), grid, dim3(256), 0, s, g);
+  else hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_kernel<false, true>), grid, dim3(256), 0, s, g);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------------------ product
+// C[M, N] = epilogue(sum_k A[m, k] B[n, k]) with v_mfma_scale_f32_16x16x128_f8f6f4: one instruction covers a block of 128, so an
+// operand's scale is one byte per row of a fragment, the same in the four lanes that share the row.  Which 32 of the 128 k a
+// lane holds is the same for A and B and does not matter otherwise.
+// The B fragment goes first: lane l then holds row l % 16 of C and columns 4 * (l / 16) + 0..3.
+//
+// How exact it is: within groups of 8 k the matrix unit drops what lies more than 13 binary places below the group's largest
+// product (measured: 2^16 + 2^2 gives 2^16; the groups, and the instructions, are added in fp32), about 1.5e-5 of a result.
+// A 16-bit result does not show it (2e-3 or 2.4e-4 of rounding); 32-bit results (EPI_ACC_F32) are therefore formed
+// with the bf16 MFMA, whose sums are exact to fp32, from codes converted in registers with their scale.
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+struct WideFrag { bf16x8 v[4]; };            // a fragment's 32 values per lane
+
+struct Fp8Args {
+  int M, N, nk;                    // nk: blocks of the contraction
+  int tiles_m, tiles_n;
+  int64_t Kp, S;
+  const uint8_t *A, *B;
+  const uint8_t *sa, *sb;
+  void* C;
+  int64_t ldc, ld_side;            // ld_side: of res or aux
+  const elem_t *bias, *res;
+  elem_t* aux;
+  int accumulate;
+};
+
+template <int J>
+__device__ __forceinline__ floatx4 mfma_fp8(intx8 b, intx8 a, floatx4 c, int sb, int sa) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, c, 0, 0, J, sb, J, sa);
+}
+
+// Byte J of a word of scales as the power of two it stands for.
+template <int J>
+__device__ __forceinline__ float scale_value(int word) { return __uint_as_float((uint32_t)(word >> 8 * J & 255) << 23); }
+__device__ __forceinline__ WideFrag widen(intx8 f, float scale) {
+  WideFrag w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    union { bf16x8 v; bf16x2 h[4]; } u;
+    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i], scale, false);
+    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i], scale, true);
+    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + 1], scale, false);
+    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(f[2 * i + 1], scale, true);
+    w.v[i] = u.v;
+  }
+  return w;
+}
+
+// Four consecutive columns n.. of row m, of which `count` exist.
+template <int EPI>
+__device__ __forceinline__ void fp8_epilogue4(const Fp8Args& g, floatx4 acc, int m, int n, bool whole) {
+  const int count = g.N - n;
+  float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+  elem_t out[4], side[4];
+  float* const cf = (float*)g.C + (int64_t)m * g.ldc + n;
+  elem_t* const ce = (elem_t*)g.C + (int64_t)m * g.ldc + n;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (!whole && e >= count) break;
+    if (EPI == EPI_BIAS || EPI == EPI_BIAS_RES || EPI == EPI_BIAS_GELU)
+      if (g.bias) v[e] += (float)g.bias[n + e];
+    if (EPI == EPI_BIAS_RES) v[e] += (float)g.res[(int64_t)m * g.ld_side + n + e];
+    if (EPI == EPI_BIAS_GELU) {
+      float y, dy;
+      gelu_with_grad_f(v[e], y, dy);
+      v[e] = y;
+      side[e] = (elem_t)dy;
+    }
+    if (EPI == EPI_DGELU) v[e] *= (float)g.aux[(int64_t)m * g.ld_side + n + e];
+    if (EPI == EPI_ACC_F32 && g.accumulate) v[e] += cf[e];
+    if (EPI == EPI_ACC_BF16 && g.accumulate) v[e] += (float)ce[e];
+    out[e] = (elem_t)v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (!whole && e >= count) break;
+    if (EPI == EPI_ACC_F32) cf[e] = v[e];
+    else ce[e] = out[e];
+    if (EPI == EPI_BIAS_GELU) g.aux[(int64_t)m * g.ld_side + n + e] = side[e];
+  }
+}
+
+// A ring of NS tiles of 128 bytes of k in LDS, filled by the memory pipeline; a wave's part of a tile is copied by the wave,
+// 8 rows of 128 bytes per instruction.  Chunk c of row r (16 bytes) lies at slot c ^ (r % 8), so that the 16 rows of a fragment
+// are read without bank conflicts.  The scales of four tiles, a word per row, are copied one round of four tiles ahead.
+template <int WM, int WN, int TM, int TN, int NS, int EPI>
+__global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_kernel(const Fp8Args g) {
+  constexpr int W = WM * WN, BM = WM * TM * 16, BN = WN * TN * 16, STAGE = (BM + BN) * FB;
+  constexpr int NA = BM / 8 / W, NB = BN / 8 / W, NC = NA + NB;      // copies of a wave per tile
+  constexpr int WS = (BM + BN) / 64, WSA = BM / 64;                  // waves that copy scales, of A
+  static_assert(BM / 8 % W == 0 && BN / 8 % W == 0 && (NS - 1) * NC < 64 && 4 % NS == 0, "copies");
+  static_assert(BM % 64 == 0 && BN % 64 == 0 && WS <= W, "scales");
+  __shared__ __align__(1024) char smem[NS * STAGE + 2 * (BM + BN) * 4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / WN, wn = wave % WN;
+  // contiguous runs of tiles for each XCD, in bands of 8 tile rows
+  int pid = blockIdx.x;
+  if ((gridDim.x & 7) == 0) pid = (pid & 7) * (gridDim.x >> 3) + (pid >> 3);
+  const int band_tiles = 8 * g.tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
+  const int rows = min(8, g.tiles_m - band * 8);
+  const int m0 = (band * 8 + in_band % rows) * BM, n0 = in_band / rows * BN;
+  const uint32_t Kp = (uint32_t)g.Kp, S = (uint32_t)g.S;
+  const uint32_t live_m = min(BM, g.M - m0), live_n = min(BN, g.N - n0);
+  const u32x4 ra = rsrc_words(g.A + (int64_t)m0 * g.Kp, live_m * Kp), rb = rsrc_words(g.B + (int64_t)n0 * g.Kp, live_n * Kp);
+  const bool scales_of_a = wave < WSA;
+  const u32x4 rs = scales_of_a ? rsrc_words(g.sa + (int64_t)m0 * g.S, live_m * S) : rsrc_words(g.sb + (int64_t)n0 * g.S, live_n * S);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(AXONN_LDS char*)smem;
+  const uint32_t at_lane = (uint32_t)(8 * wave + (lane >> 3)) * Kp + 16u * ((lane & 7) ^ (lane >> 3));
+  const uint32_t scale_lane = (uint32_t)((scales_of_a ? wave : wave - WSA) * 64 + lane) * S;
+  auto copy_tile = [&](int kt, int stage) {
+    const uint32_t k = kt < g.nk ? (uint32_t)kt * FB : 0, lds = lds0 + stage * STAGE + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < NA; ++i) dma_chunk16(ra, at_lane + (uint32_t)(8 * W * i) * Kp, k, lds + i * (W * 1024));
+#pragma unroll
+    for (int i = 0; i < NB; ++i) dma_chunk16(rb, at_lane + (uint32_t)(8 * W * i) * Kp, k, lds + BM * FB + i * (W * 1024));
+  };
+  auto copy_scales = [&](int kt) {                       // of tiles kt .. kt + 3
+    if (wave < WS && kt < g.nk) dma_word(rs, scale_lane, kt, lds0 + NS * STAGE + (kt >> 2 & 1) * ((BM + BN) * 4) + wave * 256);
+  };
+  floatx4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int r = lane & 15, q = lane >> 4;
+  const int f0 = r * FB + 16 * (q ^ (r & 7)), f1 = r * FB + 16 * ((q + 4) ^ (r & 7));
+  auto frag = [&](const char* base) {
+    union { intx8 v; u32x4 h[2]; } u;
+    u.h[0] = *reinterpret_cast<const u32x4*>(base + f0);
+    u.h[1] = *reinterpret_cast<const u32x4*>(base + f1);
+    return u.v;
+  };
+  int sa[TM] = {}, sb[TN] = {};
+  copy_scales(0);
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i) copy_tile(i, i);
+  auto load_scales = [&](int kt) {
+    const int* s = reinterpret_cast<const int*>(smem + NS * STAGE + (kt >> 2 & 1) * ((BM + BN) * 4)) + r;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] = s[(wm * TM + i) * 16];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] = s[BM + (wn * TN + j) * 16];
+  };
+  // tile kt in `stage`; `byte` of the scale words; the words are read where first says so
+  auto step = [&](auto byte, int kt, int stage, int next_stage, bool first) {
+    constexpr int J = decltype(byte)::value;
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"((NS - 2) * NC) : "memory");
+    lds_barrier();
+    if (first) {
+      copy_scales(kt + 4);
+      load_scales(kt);
+    }
+    copy_tile(kt + NS - 1, next_stage);
+    const char* tile = smem + stage * STAGE;
+    auto frag_a = [&](int i) { return frag(tile + (wm * TM + i) * 16 * FB); };
+    auto frag_b = [&](int j) { return frag(tile + BM * FB + (wn * TN + j) * 16 * FB); };
+    intx8 fa[2];
+    if constexpr (EPI == EPI_ACC_F32) {
+      WideFrag fb[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[j] = widen(frag_b(j), scale_value<J>(sb[j]));
+      fa[0] = frag_a(0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (i + 1 < TM) fa[(i + 1) & 1] = frag_a(i + 1);
+        const WideFrag wa = widen(fa[i & 1], scale_value<J>(sa[i]));
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j].v[p], wa.v[p], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      intx8 fb[TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[j] = frag_b(j);
+      fa[0] = frag_a(0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if (i + 1 < TM) fa[(i + 1) & 1] = frag_a(i + 1);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma_fp8<J>(fb[j], fa[i & 1], acc[i][j], sb[j], sa[i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  int kt = 0;
+  for (; kt + 4 <= g.nk; kt += 4) {
+    step(std::integral_constant<int, 0>{}, kt, 0, (NS - 1) % NS, true);
+    step(std::integral_constant<int, 1>{}, kt + 1, 1 % NS, NS % NS, false);
+    step(std::integral_constant<int, 2>{}, kt + 2, 2 % NS, (NS + 1) % NS, false);
+    step(std::integral_constant<int, 3>{}, kt + 3, 3 % NS, (NS + 2) % NS, false);
+  }
+  for (; kt < g.nk; ++kt) {                              // the last, shorter round: the words move instead of the immediate
+    step(std::integral_constant<int, 0>{}, kt, kt % NS, (kt + NS - 1) % NS, (kt & 3) == 0);
+#pragma unroll
+    for (int i = 0; i < TM; ++i) sa[i] >>= 8;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sb[j] >>= 8;
+  }
+  dma_wait_all();                                        // copies of tiles past the end still write to LDS
+  const bool whole = n0 + BN <= g.N;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + (wm * TM + i) * 16 + r;
+    if (m >= g.M) continue;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int n = n0 + (wn * TN + j) * 16 + 4 * q;
+      if (n < g.N) fp8_epilogue4<EPI>(g, acc[i][j], m, n, whole);
+    }
+  }
+}
+
+template <int WM, int WN, int TM, int TN, int NS, int EPI>
+static hipError_t launch_fp8_tile(Fp8Args g, hipStream_t s) {
+  constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
+  g.tiles_m = (g.M + BM - 1) / BM;
+  g.tiles_n = (g.N + BN - 1) / BN;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_kernel<WM, WN, TM, TN, NS, EPI>), dim3((unsigned)(g.tiles_m * g.tiles_n)),
+                     dim3(64 * WM * WN), 0, s, g);
+  return hipGetLastError();
+}
+template <int EPI>
+static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
+  auto tiles = [&](int64_t bm, int64_t bn) { return (g.M + bm - 1) / bm * ((g.N + bn - 1) / bn); };
+  if (tiles(256, 256) >= 256) {
+    if constexpr (EPI == EPI_ACC_F32) return launch_fp8_tile<2, 4, 4, 4, 2, EPI>(g, s);
+    else return launch_fp8_tile<2, 4, 8, 4, 2, EPI>(g, s);
+  }
+  if (tiles(128, 128) >= 192) return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
+  return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
+}
+
+hipError_t launch_gemm_fp8(int epi, int64_t M, int64_t N, int64_t K, const void* A, const void* a_scale, const void* B, const void* b_scale,
+                           void* C, int64_t ldc, const void* bias, const void* res, int64_t ld_res, void* aux, int64_t ld_aux,
+                           int accumulate, hipStream_t s) {
+  Fp8Args g = {};
+  g.M = (int)M; g.N = (int)N; g.nk = (int)((K + FB - 1) / FB);
+  g.Kp = (int64_t)g.nk * FB; g.S = (g.nk + 3) / 4 * 4;
+  g.A = (const uint8_t*)A; g.B = (const uint8_t*)B; g.sa = (const uint8_t*)a_scale; g.sb = (const uint8_t*)b_scale;
+  g.C = C; g.ldc = ldc; g.ld_side = epi == EPI_BIAS_RES ? ld_res : ld_aux;
+  g.bias = (const elem_t*)bias; g.res = (const elem_t*)res; g.aux = (elem_t*)aux; g.accumulate = accumulate;
+  switch (epi) {
+    case EPI_BIAS: return launch_fp8<EPI_BIAS>(g, s);
+    case EPI_BIAS_RES: return launch_fp8<EPI_BIAS_RES>(g, s);
+    case EPI_BIAS_GELU: return launch_fp8<EPI_BIAS_GELU>(g, s);
+    case EPI_DGELU: return launch_fp8<EPI_DGELU>(g, s);
+    case EPI_ACC_F32: return launch_fp8<EPI_ACC_F32>(g, s);
+    default: return launch_fp8<EPI_ACC_BF16>(g, s);
+  }
+}
+
+}  // namespace axonn
