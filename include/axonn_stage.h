@@ -552,7 +552,7 @@ int axonn_dropout_bwd(int64_t T, int64_t h, const void* dout_bf16, int64_t ld_do
  * a scale for each block of 128 elements along the contraction.  The scale is the least power of
  * two 2^e, e >= -127, with which the block's largest finite magnitude is at most 448 * 2^e, stored
  * as the byte e + 127 (0 for a block of zeros); a code is x / 2^e rounded to nearest, ties to even.
- * An infinity or NaN becomes the code of NaN and has no part in the scale.
+ * An infinity or NaN becomes 0x7f, the format's NaN, and has no part in the scale.
  * A form of a matrix with rows of K elements: codes [rows][Kp], Kp = 128 * ceil(K / 128), zeros
  * behind K; scales [rows][4 * ceil(Kp / 512)], zeros behind the last block.
  * x [R, C]: q, scale receive its rows (blocks along C), q_t, scale_t the rows of its transpose

@@ -15,7 +15,8 @@ no buckets, no streams, no tiling.
 
 Modules: transformer (layers, stage, activation checkpointing of Sec. 5.1 with Eq. 1 and
 the stride rule), lm_ends (first stage's embedding; last stage's final LayerNorm, LM head
-and pre-divided loss, Alg. 2 / Sec. 4.2), adam.
+and pre-divided loss, Alg. 2 / Sec. 4.2), adam, step_ops (operations of a training step around
+the layer's own: scaled embedding, query / key norms with rotation, dropout, 8-bit matrices).
 
 Parity pins (see tests/test_oracle_*.py): every gradient formula is pinned by central
 finite differences; softmax, LayerNorm, GeLU, the linear maps, the loss and Adam are

@@ -26,7 +26,7 @@ __device__ __forceinline__ float finite_magnitude(float v) {
   const float a = fabsf(v);
   return a < INFINITY ? a : 0.f;             // an infinity or NaN has no part in the scale
 }
-// Codes of four values, the first in the low byte; an infinity or NaN becomes the code of NaN.
+// Codes of four values, the first in the low byte; an infinity or NaN becomes 0x7f.
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float inv) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
   w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
@@ -35,7 +35,7 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, 
   if (!(fabsf(b) < INFINITY)) bad |= 0x7f00u;
   if (!(fabsf(c) < INFINITY)) bad |= 0x7f0000u;
   if (!(fabsf(d) < INFINITY)) bad |= 0x7f000000u;
-  return (uint32_t)w | bad;
+  return ((uint32_t)w | bad) & ~((bad & 0x40404040u) << 1);      // 0x7f, whatever the sign was
 }
 
 struct QuantArgs {
