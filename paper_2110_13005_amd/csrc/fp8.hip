@@ -196,37 +196,85 @@ __device__ __forceinline__ WideFrag widen(intx8 f, float scale) {
   return w;
 }
 
-// Four consecutive columns n.. of row m, of which `count` exist.
+// Columns n .. n + count of row m, count <= 8: v = the sums, bv = their bias.
 template <int EPI>
-__device__ __forceinline__ void fp8_epilogue4(const Fp8Args& g, floatx4 acc, int m, int n, bool whole) {
-  const int count = g.N - n;
-  float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-  elem_t out[4], side[4];
-  float* const cf = (float*)g.C + (int64_t)m * g.ldc + n;
-  elem_t* const ce = (elem_t*)g.C + (int64_t)m * g.ldc + n;
+__device__ __forceinline__ void fp8_epilogue8(const Fp8Args& g, float (&v)[8], const float (&bv)[8], int m, int n, int count) {
+  if constexpr (EPI == EPI_ACC_F32) {
+    float* p = (float*)g.C + (int64_t)m * g.ldc + n;
+    if (count >= 8) {
+      typedef floatx4 floatx4_any __attribute__((aligned(4)));
+      floatx4_any* pv = (floatx4_any*)p;
+      floatx4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+      if (g.accumulate) { lo += pv[0]; hi += pv[1]; }
+      pv[0] = lo;
+      pv[1] = hi;
+    } else {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (!whole && e >= count) break;
-    if (EPI == EPI_BIAS || EPI == EPI_BIAS_RES || EPI == EPI_BIAS_GELU)
-      if (g.bias) v[e] += (float)g.bias[n + e];
-    if (EPI == EPI_BIAS_RES) v[e] += (float)g.res[(int64_t)m * g.ld_side + n + e];
-    if (EPI == EPI_BIAS_GELU) {
+      for (int e = 0; e < 7; ++e)
+        if (e < count) p[e] = v[e] + (g.accumulate ? p[e] : 0.f);
+    }
+    return;
+  }
+  elem_t* const c = (elem_t*)g.C + (int64_t)m * g.ldc + n;
+  elemx8 x = {}, out;
+  if (EPI == EPI_BIAS_RES) x = load_chunk(g.res + (int64_t)m * g.ld_side + n, count);
+  if (EPI == EPI_DGELU) x = load_chunk(g.aux + (int64_t)m * g.ld_side + n, count);
+  if (EPI == EPI_ACC_BF16 && g.accumulate) x = load_chunk(c, count);
+  if (EPI == EPI_BIAS || EPI == EPI_BIAS_RES || EPI == EPI_BIAS_GELU) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += bv[e];
+  }
+  if (EPI == EPI_BIAS_GELU) {
+    elemx8 dv;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
       float y, dy;
       gelu_with_grad_f(v[e], y, dy);
       v[e] = y;
-      side[e] = (elem_t)dy;
+      dv[e] = (elem_t)dy;
     }
-    if (EPI == EPI_DGELU) v[e] *= (float)g.aux[(int64_t)m * g.ld_side + n + e];
-    if (EPI == EPI_ACC_F32 && g.accumulate) v[e] += cf[e];
-    if (EPI == EPI_ACC_BF16 && g.accumulate) v[e] += (float)ce[e];
-    out[e] = (elem_t)v[e];
+    store_chunk(g.aux + (int64_t)m * g.ld_side + n, dv, count);
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (!whole && e >= count) break;
-    if (EPI == EPI_ACC_F32) cf[e] = v[e];
-    else ce[e] = out[e];
-    if (EPI == EPI_BIAS_GELU) g.aux[(int64_t)m * g.ld_side + n + e] = side[e];
+  for (int e = 0; e < 8; ++e) {
+    if (EPI == EPI_DGELU) v[e] *= (float)x[e];
+    if (EPI == EPI_BIAS_RES || EPI == EPI_ACC_BF16) v[e] += (float)x[e];
+    out[e] = (elem_t)v[e];
+  }
+  store_chunk(c, out, count);
+}
+
+// A wave's TM x TN result tiles at (m0, n0), IP tile rows at a time through `stage`, the wave's own part of LDS
+// (16 * IP rows of 16 * TN + 4 floats: conflict-free both ways).  Straight from the MFMA's layout an instruction would touch 16
+// rows with 32 bytes each; from LDS it stores rows of up to 256 bytes.
+template <int EPI, int TM, int TN, int IP>
+__device__ __forceinline__ void fp8_epilogue(const Fp8Args& g, const floatx4 (&acc)[TM][TN], float* stage, int m0, int n0, int lane) {
+  constexpr int LD = 16 * TN + 4, LPR = 2 * TN, RPI = 64 / LPR;      // lanes of a row, rows of an instruction
+  const int n = n0 + 8 * (lane % LPR), count = g.N - n;
+  float bv[8];
+  {
+    elemx8 b = {};
+    if ((EPI == EPI_BIAS || EPI == EPI_BIAS_RES || EPI == EPI_BIAS_GELU) && g.bias && count > 0) b = load_chunk(g.bias + n, count);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bv[e] = (float)b[e];
+  }
+#pragma unroll
+  for (int i0 = 0; i0 < TM; i0 += IP) {
+#pragma unroll
+    for (int i = 0; i < IP; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        *reinterpret_cast<floatx4*>(stage + (16 * i + (lane & 15)) * LD + 16 * j + 4 * (lane >> 4)) = acc[i0 + i][j];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+    for (int t = 0; t < 16 * IP; t += RPI) {
+      const int row = t + lane / LPR, m = m0 + 16 * i0 + row;
+      const floatx4* s = reinterpret_cast<const floatx4*>(stage + row * LD + 8 * (lane % LPR));
+      const floatx4 lo = s[0], hi = s[1];
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      if (m < g.M && count > 0) fp8_epilogue8<EPI>(g, v, bv, m, n, count);
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -350,19 +398,175 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_kernel(const Fp8Args g)
     for (int j = 0; j < TN; ++j) sb[j] >>= 8;
   }
   dma_wait_all();                                        // copies of tiles past the end still write to LDS
-  const bool whole = n0 + BN <= g.N;
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int m = m0 + (wm * TM + i) * 16 + r;
-    if (m >= g.M) continue;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int n = n0 + (wn * TN + j) * 16 + 4 * q;
-      if (n < g.N) fp8_epilogue4<EPI>(g, acc[i][j], m, n, whole);
-    }
-  }
+  lds_barrier();
+  constexpr int IP = TM < 2 ? TM : 2;
+  static_assert(W * 16 * IP * (16 * TN + 4) * 4 <= (int)sizeof smem, "staging");
+  fp8_epilogue<EPI, TM, TN, IP>(g, acc, (float*)smem + wave * (16 * IP * (16 * TN + 4)), m0 + wm * TM * 16, n0 + wn * TN * 16, lane);
 }
 
+// The product for problems that fill the chip with 256 x 256 tiles: four waves, one per SIMD, each 128 x 128 of the result, the
+// 256 accumulators in the accumulation registers.  With 8 waves of 128 x 64 (196 KB of fragments per tile of k instead of 128 KB,
+// and every wave at the barrier with nothing to do) the product of 8192 x 5120 x 20480 took 1000 us.
+//
+// Half a tile of k (the rows of four of the eight fragments) is the unit of copying: a set holds half of A(kt) and half of
+// B(kt + 1), 16 KB each, four sets in LDS.  A group is the 8 MFMAs of one A fragment; while it runs, the next A fragment and one B
+// fragment of the next tile are read, so B's fragments are in registers a tile ahead and no group waits for LDS.  The last
+// group of a half runs behind the barrier that opens the next set, which was copied one and a half tiles of k ago.
+// J: which byte of a scale's register.
+template <int J>
+__device__ __forceinline__ void mfma_fp8_acc(floatx4& c, intx8 b, intx8 a, int sb, int sa) {
+  if constexpr (J == 0)
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+  else
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0]"
+                 : "+a"(c) : "v"(b), "v"(a), "v"(sb), "v"(sa));
+}
+
+template <int EPI>
+__global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
+  constexpr int BM = 256, BN = 256, HALF = 128 * FB, SET = 2 * HALF, SCALES = 4 * SET, SBUF = (BM + BN) * 4;
+  __shared__ __align__(1024) char smem[SCALES + 2 * SBUF];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  int pid = blockIdx.x;
+  if ((gridDim.x & 7) == 0) pid = (pid & 7) * (gridDim.x >> 3) + (pid >> 3);
+  const int band_tiles = 8 * g.tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
+  const int rows = min(8, g.tiles_m - band * 8);
+  const int m0 = (band * 8 + in_band % rows) * BM, n0 = in_band / rows * BN;
+  const uint32_t Kp = (uint32_t)g.Kp, S = (uint32_t)g.S;
+  const uint32_t live_m = min(BM, g.M - m0), live_n = min(BN, g.N - n0);
+  u32x4 ra = rsrc_words(g.A + (int64_t)m0 * g.Kp, live_m * Kp), rb = rsrc_words(g.B + (int64_t)n0 * g.Kp, live_n * Kp);
+  const u32x4 rsa = rsrc_words(g.sa + (int64_t)m0 * g.S, live_m * S), rsb = rsrc_words(g.sb + (int64_t)n0 * g.S, live_n * S);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(AXONN_LDS char*)smem;
+  // copies: rows 32 * wave .. + 31 of a half, whose 128 rows are rows 64 h .. + 63 of both waves' 128
+  const uint32_t from = ((uint32_t)(wave >> 1) * 128 + (wave & 1) * 32 + (lane >> 3)) * Kp + 16u * ((lane & 7) ^ (lane >> 3));
+  const uint32_t scale_from = (uint32_t)(64 * wave + lane) * S;
+  // copy c of 0..7: four of A(kt), then four of B(kt + 1); tiles past the end read nothing (their descriptors are empty)
+  auto aim = [&](int kt) {
+    ra[2] = kt < g.nk ? live_m * Kp : 0;
+    rb[2] = kt + 1 < g.nk ? live_n * Kp : 0;
+  };
+  auto copy = [&](int kt, int h, int slot, int c) {
+    dma_chunk16(c < 4 ? ra : rb, from + (uint32_t)(64 * h + 8 * (c & 3)) * Kp, (uint32_t)(c < 4 ? kt : kt + 1) * FB,
+                lds0 + slot * SET + (c < 4 ? 0 : HALF) + wave * 4096 + (c & 3) * 1024);
+  };
+  auto copy_scales = [&](int kt) {                       // of tiles kt .. kt + 3
+    const uint32_t to = lds0 + SCALES + (kt >> 2 & 1) * SBUF + wave * 256;
+    if (kt >= g.nk) return;
+    dma_word(rsa, scale_from, kt, to);
+    dma_word(rsb, scale_from, kt, to + BM * 4);
+  };
+  floatx4 acc[8][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  const int r = lane & 15, q = lane >> 4;
+  const int f0 = r * FB + 16 * (q ^ (r & 7)), f1 = r * FB + 16 * ((q + 4) ^ (r & 7));
+  const char* const a0 = smem + wm * (64 * FB) + f0;     // fragment k of a set's A: + slot * SET + k * 16 * FB
+  const char* const a1 = smem + wm * (64 * FB) + f1;
+  const char* const b0 = smem + HALF + wn * (64 * FB) + f0;
+  const char* const b1 = smem + HALF + wn * (64 * FB) + f1;
+  const char* const sca = smem + SCALES + wm * 512 + 4 * r;      // a fragment's scales: + 64 bytes each
+  const char* const scb = smem + SCALES + BM * 4 + wn * 512 + 4 * r;
+  auto scale_at = [](int t) { return (t >> 2 & 1) * SBUF + (t & 2); };             // of tile t and its neighbour
+  union Frag { intx8 v; u32x4 h[2]; };
+  Frag fa[2], fb[2][8];
+  int sa[2], sb[2][8];
+  // A scale as loaded (16 bits, the rest zero): without this the compiler clears the rest again in front of the MFMA, where nobody
+  // keeps the distance from a vector instruction to the MFMA that reads its result.
+#define AXONN_AS_LOADED(x) asm volatile("" : "+v"(x))
+
+  copy_scales(0);
+  aim(-1);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)                            // B(0): the second halves of sets -2 and -1
+#pragma unroll
+    for (int c = 4; c < 8; ++c) copy(-1, h, 2 + h, c);
+  aim(0);
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) copy(0, h, h, c);
+  asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+  lds_barrier();
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    fb[0][j].h[0] = *reinterpret_cast<const u32x4*>(b0 + (2 + (j >> 2)) * SET + (j & 3) * 16 * FB);
+    fb[0][j].h[1] = *reinterpret_cast<const u32x4*>(b1 + (2 + (j >> 2)) * SET + (j & 3) * 16 * FB);
+    sb[0][j] = *reinterpret_cast<const uint16_t*>(scb + scale_at(0) + j * 64);
+    AXONN_AS_LOADED(sb[0][j]);
+  }
+  lds_barrier();
+  aim(1);
+#pragma unroll
+  for (int c = 0; c < 8; ++c) copy(1, 0, 2, c);
+  asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+  lds_barrier();
+#pragma unroll
+  for (int c = 0; c < 8; ++c) copy(1, 1, 3, c);
+  fa[0].h[0] = *reinterpret_cast<const u32x4*>(a0);
+  fa[0].h[1] = *reinterpret_cast<const u32x4*>(a1);
+  sa[0] = *reinterpret_cast<const uint16_t*>(sca + scale_at(0));
+  fb[1][0].h[0] = *reinterpret_cast<const u32x4*>(b0);
+  fb[1][0].h[1] = *reinterpret_cast<const u32x4*>(b1);
+  sb[1][0] = *reinterpret_cast<const uint16_t*>(scb + scale_at(1));
+  AXONN_AS_LOADED(sa[0]);
+  AXONN_AS_LOADED(sb[1][0]);
+  __builtin_amdgcn_sched_barrier(0);
+
+  // tile kt = 2 * round + J: fragments of A in turn; what is read belongs to the next fragment, a tile later behind the last one
+  auto step = [&](auto parity, int kt) {
+    constexpr int J = decltype(parity)::value;
+    const char* const sa_now = sca + scale_at(kt);
+    const char* const sa_next = sca + scale_at(kt + 1);
+    const char* const sb_now = scb + scale_at(kt + 1);
+    const char* const sb_next = scb + scale_at(kt + 2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const bool last = i == 7, opens = (i & 3) == 3;
+      const int h = opens ? (i >> 2) ^ 1 : i >> 2;        // half of the set that is read
+      const int k = (i + 1) & 3, slot = (2 * J + (last ? 2 : h)) & 3;
+      const int nb = last ? J : J ^ 1;                    // the B fragment read belongs to the next tile, or the one behind it
+      if (opens) {
+        asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+        lds_barrier();
+        if (i == 3) aim(kt + 2);
+        if (i == 3 && (kt & 3) == 0) copy_scales(kt + 4);
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        mfma_fp8_acc<J>(acc[i][j], fb[J][j].v, fa[i & 1].v, sb[J][j], sa[i & 1]);
+        if (j == 0) fa[(i + 1) & 1].h[0] = *reinterpret_cast<const u32x4*>(a0 + slot * SET + k * 16 * FB);
+        if (j == 1) fa[(i + 1) & 1].h[1] = *reinterpret_cast<const u32x4*>(a1 + slot * SET + k * 16 * FB);
+        if (j == 2) sa[(i + 1) & 1] = *reinterpret_cast<const uint16_t*>((last ? sa_next : sa_now) + ((i + 1) & 7) * 64);
+        if (j == 3) sb[nb][4 * h + k] = *reinterpret_cast<const uint16_t*>((last ? sb_next : sb_now) + (4 * h + k) * 64);
+        if (j == 4) fb[nb][4 * h + k].h[0] = *reinterpret_cast<const u32x4*>(b0 + slot * SET + k * 16 * FB);
+        if (j == 5) fb[nb][4 * h + k].h[1] = *reinterpret_cast<const u32x4*>(b1 + slot * SET + k * 16 * FB);
+        if (j == 7) {
+          AXONN_AS_LOADED(sa[(i + 1) & 1]);
+          AXONN_AS_LOADED(sb[nb][4 * h + k]);
+        }
+        if (opens) copy(kt + 2, i >> 2, (2 * J + (i >> 2)) & 3, j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  };
+  // an odd number of tiles: one more, of zeros
+  int kt = 0;
+  do {
+    step(std::integral_constant<int, 0>{}, kt);
+    step(std::integral_constant<int, 1>{}, kt + 1);
+    kt += 2;
+  } while (kt < g.nk);
+#undef AXONN_AS_LOADED
+  // the matrix unit's last results; the compiler does not know what wrote them
+  asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+  dma_wait_all();                                        // copies of tiles past the end still write (zeros) to LDS
+  lds_barrier();
+  static_assert(4 * 64 * 132 * 4 <= (int)sizeof smem, "staging");
+  fp8_epilogue<EPI, 8, 8, 4>(g, acc, (float*)smem + wave * (64 * 132), m0 + wm * 128, n0 + wn * 128, lane);
+}
 template <int WM, int WN, int TM, int TN, int NS, int EPI>
 static hipError_t launch_fp8_tile(Fp8Args g, hipStream_t s) {
   constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
@@ -373,11 +577,18 @@ static hipError_t launch_fp8_tile(Fp8Args g, hipStream_t s) {
   return hipGetLastError();
 }
 template <int EPI>
+static hipError_t launch_fp8_big(Fp8Args g, hipStream_t s) {
+  g.tiles_m = (g.M + 255) / 256;
+  g.tiles_n = (g.N + 255) / 256;
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_big_kernel<EPI>), dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(256), 0, s, g);
+  return hipGetLastError();
+}
+template <int EPI>
 static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
   auto tiles = [&](int64_t bm, int64_t bn) { return (g.M + bm - 1) / bm * ((g.N + bn - 1) / bn); };
   if (tiles(256, 256) >= 256) {
     if constexpr (EPI == EPI_ACC_F32) return launch_fp8_tile<2, 4, 4, 4, 2, EPI>(g, s);
-    else return launch_fp8_tile<2, 4, 8, 4, 2, EPI>(g, s);
+    else return launch_fp8_big<EPI>(g, s);
   }
   if (tiles(128, 128) >= 192) return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
   return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);

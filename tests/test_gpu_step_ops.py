@@ -598,3 +598,43 @@ def test_a_training_step_of_a_layers_attention_half():
                               ("dgq", dgq, 5), ("dgk", dgk, 5), ("du", du, 5), ("dw_qkv", dw_qkv, 5), ("dx", dx, 5), ("demb", demb, 5),
                               ("dtable", dtable, 5)):
         assert rel_fro(got[name], ref) <= max(2 * half_step(), passed * one), (name, rel_fro(got[name], ref))
+
+
+@pytest.mark.parametrize("M,N,K", [(4096, 4096, 100), (4096, 4096, 130), (3841, 4356, 300), (4096, 4096, 512), (4100, 4200, 600), (4096, 4096, 1030),
+                                   (4352, 4096, 1500)])
+def test_large_products_of_every_length(M, N, K):
+    """Products that fill the chip, over contractions of one block of k and more, an odd number of them too; a result of each
+    kind of rounding.  The float64 sums are formed on the GPU from the values that the oracle says the codes stand for."""
+    import torch
+    rng = np.random.default_rng(K)
+    forms = []
+    for rows in (M, N):
+        codes = rng.integers(0, 256, (rows, -(-K // 128) * 128)).astype(np.uint8)
+        codes[(codes & 0x7f) == 0x7f] = 0
+        codes[:, K:] = 0
+        scales = np.zeros((rows, -(-K // 512) * 4), np.uint8)
+        nb = -(-K // 128)
+        scales[:, :nb] = rng.integers(110, 140, (rows, nb))
+        forms += [codes, scales]
+    dev = [torch.from_numpy(f).cuda() for f in forms]
+    values = torch.from_numpy(O.e4m3_values()).cuda().nan_to_num(0.0)
+
+    def stands_for(codes, scales):
+        e = scales[:, :codes.shape[1] // 128].double() - 127.0
+        return values[codes.long()] * torch.exp2(e).repeat_interleave(128, dim=1)
+    a, b = stands_for(*dev[:2]), stands_for(*dev[2:])
+    # brought into half precision's range by the scales of A
+    shift = int(torch.log2((a @ b.t()).abs().max()).item()) - 12
+    dev[1].sub_((dev[1] > 0).to(torch.uint8) * shift if shift >= 0 else -(dev[1] > 0).to(torch.uint8) * (-shift))
+    a = a * 2.0 ** -shift
+    ref, mags = a @ b.t(), a.abs() @ b.abs().t()
+    for epi, dt in ((B.EPI_BIAS, B.torch_elem_dtype()), (B.EPI_ACC_F32, torch.float32)):
+        wide = dt == torch.float32
+        C = torch.full((M + 1, N), 7.0, dtype=dt, device="cuda")
+        B.axonn_gemm_fp8(epi, M, N, K, *dev, C, N)
+        half = U if wide else half_step()
+        slack = _product_slack(mags, K, wide)
+        err = (C[:M].double() - ref).abs()
+        assert bool((err <= half * (ref.abs() + slack) + slack + 2.0 ** -25).all()), float((err / (slack + half * ref.abs())).max())
+        assert float(err.norm() / ref.norm()) <= 0.64 * half + (K + 8) * U
+        assert bool((C[M] == 7.0).all())
