@@ -245,11 +245,11 @@ __device__ __forceinline__ void fp8_epilogue8(const Fp8Args& g, float (&v)[8], c
 }
 
 // A wave's TM x TN result tiles at (m0, n0), IP tile rows at a time through `stage`, the wave's own part of LDS
-// (16 * IP rows of 16 * TN + 4 floats: conflict-free both ways).  Straight from the MFMA's layout an instruction would touch 16
-// rows with 32 bytes each; from LDS it stores rows of up to 256 bytes.
+// (16 * IP rows of 16 * TN floats, 16-byte chunk c of row r at c ^ (r % 8): conflict-free both ways).  Straight from the MFMA's
+// layout an instruction would touch 16 rows with 32 bytes each; from LDS it stores rows of up to 256 bytes.
 template <int EPI, int TM, int TN, int IP>
 __device__ __forceinline__ void fp8_epilogue(const Fp8Args& g, const floatx4 (&acc)[TM][TN], float* stage, int m0, int n0, int lane) {
-  constexpr int LD = 16 * TN + 4, LPR = 2 * TN, RPI = 64 / LPR;      // lanes of a row, rows of an instruction
+  constexpr int LD = 16 * TN, LPR = 2 * TN, RPI = 64 / LPR;          // lanes of a row, rows of an instruction
   const int n = n0 + 8 * (lane % LPR), count = g.N - n;
   float bv[8];
   {
@@ -264,18 +264,27 @@ __device__ __forceinline__ void fp8_epilogue(const Fp8Args& g, const floatx4 (&a
     for (int i = 0; i < IP; ++i)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
-        *reinterpret_cast<floatx4*>(stage + (16 * i + (lane & 15)) * LD + 16 * j + 4 * (lane >> 4)) = acc[i0 + i][j];
+        *reinterpret_cast<floatx4*>(stage + (16 * i + (lane & 15)) * LD + 4 * ((4 * j + (lane >> 4)) ^ (lane & 7))) = acc[i0 + i][j];
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 4
+#pragma unroll
     for (int t = 0; t < 16 * IP; t += RPI) {
-      const int row = t + lane / LPR, m = m0 + 16 * i0 + row;
-      const floatx4* s = reinterpret_cast<const floatx4*>(stage + row * LD + 8 * (lane % LPR));
-      const floatx4 lo = s[0], hi = s[1];
+      const int row = t + lane / LPR, m = m0 + 16 * i0 + row, c = 2 * (lane % LPR);
+      const float* s = stage + row * LD;
+      const floatx4 lo = *reinterpret_cast<const floatx4*>(s + 4 * (c ^ (row & 7)));
+      const floatx4 hi = *reinterpret_cast<const floatx4*>(s + 4 * ((c + 1) ^ (row & 7)));
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       if (m < g.M && count > 0) fp8_epilogue8<EPI>(g, v, bv, m, n, count);
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+// Tile of a workgroup: contiguous runs of tiles for each XCD (workgroups go round the eight), in bands of 8 tile rows.
+__device__ __forceinline__ void fp8_tile_at(int pid, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int band_tiles = 8 * tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
+  const int rows = min(8, tiles_m - band * 8);
+  tm = band * 8 + in_band % rows;
+  tn = in_band / rows;
 }
 
 // A ring of NS tiles of 128 bytes of k in LDS, filled by the memory pipeline; a wave's part of a tile is copied by the wave,
@@ -291,12 +300,10 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_kernel(const Fp8Args g)
   __shared__ __align__(1024) char smem[NS * STAGE + 2 * (BM + BN) * 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WN, wn = wave % WN;
-  // contiguous runs of tiles for each XCD, in bands of 8 tile rows
-  int pid = blockIdx.x;
+  int pid = blockIdx.x, tm, tn;
   if ((gridDim.x & 7) == 0) pid = (pid & 7) * (gridDim.x >> 3) + (pid >> 3);
-  const int band_tiles = 8 * g.tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
-  const int rows = min(8, g.tiles_m - band * 8);
-  const int m0 = (band * 8 + in_band % rows) * BM, n0 = in_band / rows * BN;
+  fp8_tile_at(pid, g.tiles_m, g.tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
   const uint32_t Kp = (uint32_t)g.Kp, S = (uint32_t)g.S;
   const uint32_t live_m = min(BM, g.M - m0), live_n = min(BN, g.N - n0);
   const u32x4 ra = rsrc_words(g.A + (int64_t)m0 * g.Kp, live_m * Kp), rb = rsrc_words(g.B + (int64_t)n0 * g.Kp, live_n * Kp);
@@ -400,18 +407,24 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_kernel(const Fp8Args g)
   dma_wait_all();                                        // copies of tiles past the end still write to LDS
   lds_barrier();
   constexpr int IP = TM < 2 ? TM : 2;
-  static_assert(W * 16 * IP * (16 * TN + 4) * 4 <= (int)sizeof smem, "staging");
-  fp8_epilogue<EPI, TM, TN, IP>(g, acc, (float*)smem + wave * (16 * IP * (16 * TN + 4)), m0 + wm * TM * 16, n0 + wn * TN * 16, lane);
+  static_assert(W * 16 * IP * 16 * TN * 4 <= (int)sizeof smem, "staging");
+  fp8_epilogue<EPI, TM, TN, IP>(g, acc, (float*)smem + wave * (16 * IP * 16 * TN), m0 + wm * TM * 16, n0 + wn * TN * 16, lane);
 }
 
 // The product for problems that fill the chip with 256 x 256 tiles: four waves, one per SIMD, each 128 x 128 of the result, the
 // 256 accumulators in the accumulation registers.  With 8 waves of 128 x 64 (196 KB of fragments per tile of k instead of 128 KB,
-// and every wave at the barrier with nothing to do) the product of 8192 x 5120 x 20480 took 1000 us.
+// and every wave at the barrier with nothing to do) the product of 8192 x 5120 x 20480 took 1000 us, this way 725 (2370 TFLOP/s;
+// 8192^3 381 us, 2880).  The matrix units are busy 77 % of the cycles there, at the 1.75 GHz that the chip's power leaves (zeros for
+// operands: 3200).
 //
 // Half a tile of k (the rows of four of the eight fragments) is the unit of copying: a set holds half of A(kt) and half of
 // B(kt + 1), 16 KB each, four sets in LDS.  A group is the 8 MFMAs of one A fragment; while it runs, the next A fragment and one B
 // fragment of the next tile are read, so B's fragments are in registers a tile ahead and no group waits for LDS.  The last
 // group of a half runs behind the barrier that opens the next set, which was copied one and a half tiles of k ago.
+//
+// A workgroup does one tile of the result after the other, and what is copied and read ahead at the end of one belongs to the
+// next: its first sets arrive while the epilogue stores.  The epilogue has the LDS of one set, whose copy waits until it is done.
+// The steps of a tile are rounded up to four (a word of scales), the ones past the end on zeros.
 // J: which byte of a scale's register.
 template <int J>
 __device__ __forceinline__ void mfma_fp8_acc(floatx4& c, intx8 b, intx8 a, int sb, int sa) {
@@ -428,39 +441,56 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
   __shared__ __align__(1024) char smem[SCALES + 2 * SBUF];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  int pid = blockIdx.x;
-  if ((gridDim.x & 7) == 0) pid = (pid & 7) * (gridDim.x >> 3) + (pid >> 3);
-  const int band_tiles = 8 * g.tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
-  const int rows = min(8, g.tiles_m - band * 8);
-  const int m0 = (band * 8 + in_band % rows) * BM, n0 = in_band / rows * BN;
   const uint32_t Kp = (uint32_t)g.Kp, S = (uint32_t)g.S;
-  const uint32_t live_m = min(BM, g.M - m0), live_n = min(BN, g.N - n0);
-  u32x4 ra = rsrc_words(g.A + (int64_t)m0 * g.Kp, live_m * Kp), rb = rsrc_words(g.B + (int64_t)n0 * g.Kp, live_n * Kp);
-  const u32x4 rsa = rsrc_words(g.sa + (int64_t)m0 * g.S, live_m * S), rsb = rsrc_words(g.sb + (int64_t)n0 * g.S, live_n * S);
+  const int steps = (g.nk + 3) & ~3;
+  // this workgroup's tiles: a run of each XCD's share
+  const int n_tiles = g.tiles_m * g.tiles_n, xcds = (gridDim.x & 7) == 0 ? 8 : 1;
+  const int share = (n_tiles + xcds - 1) / xcds, stride = gridDim.x / xcds;
+  const int first = blockIdx.x % xcds * share, end = min(n_tiles, first + share);
+  int pid = first + blockIdx.x / xcds;
+  if (pid >= end) return;
+  struct Tile { int m0, n0; };                           // past the last one: behind the matrix, where nothing is read
+  auto tile_of = [&](int p) {
+    Tile t = {g.M, g.N};
+    if (p < end) {
+      int tm, tn;
+      fp8_tile_at(p, g.tiles_m, g.tiles_n, tm, tn);
+      t.m0 = __builtin_amdgcn_readfirstlane(tm * BM);
+      t.n0 = __builtin_amdgcn_readfirstlane(tn * BN);
+    }
+    return t;
+  };
+  // descriptor of the rows of a matrix (`ld` bytes each) from m0 on, `most` of them at most; empty unless `live`
+  auto rows_of = [](const uint8_t* p, int m0, int n_rows, int most, uint32_t ld, bool live) {
+    return rsrc_words(p + (int64_t)m0 * ld, live ? (uint32_t)min(most, n_rows - m0) * ld : 0);
+  };
+  Tile now = tile_of(pid), next = tile_of(pid + stride);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(AXONN_LDS char*)smem;
   // copies: rows 32 * wave .. + 31 of a half, whose 128 rows are rows 64 h .. + 63 of both waves' 128
   const uint32_t from = ((uint32_t)(wave >> 1) * 128 + (wave & 1) * 32 + (lane >> 3)) * Kp + 16u * ((lane & 7) ^ (lane >> 3));
   const uint32_t scale_from = (uint32_t)(64 * wave + lane) * S;
-  // copy c of 0..7: four of A(kt), then four of B(kt + 1); tiles past the end read nothing (their descriptors are empty)
+  // copy c of 0..7 of step kt: four of A(kt), then four of B(kt + 1); aim() sets where from, steps past the tile's are the next's
+  u32x4 ra, rb;
+  uint32_t ka, kb;
   auto aim = [&](int kt) {
-    ra[2] = kt < g.nk ? live_m * Kp : 0;
-    rb[2] = kt + 1 < g.nk ? live_n * Kp : 0;
+    const int ta = kt < steps ? kt : kt - steps, tb = kt + 1 < steps ? kt + 1 : kt + 1 - steps;
+    ra = rows_of(g.A, kt < steps ? now.m0 : next.m0, g.M, BM, Kp, ta < g.nk);
+    rb = rows_of(g.B, kt + 1 < steps ? now.n0 : next.n0, g.N, BN, Kp, tb < g.nk);
+    ka = (uint32_t)ta * FB;
+    kb = (uint32_t)tb * FB;
   };
-  auto copy = [&](int kt, int h, int slot, int c) {
-    dma_chunk16(c < 4 ? ra : rb, from + (uint32_t)(64 * h + 8 * (c & 3)) * Kp, (uint32_t)(c < 4 ? kt : kt + 1) * FB,
+  auto copy = [&](int h, int slot, int c) {
+    dma_chunk16(c < 4 ? ra : rb, from + (uint32_t)(64 * h + 8 * (c & 3)) * Kp, c < 4 ? ka : kb,
                 lds0 + slot * SET + (c < 4 ? 0 : HALF) + wave * 4096 + (c & 3) * 1024);
   };
-  auto copy_scales = [&](int kt) {                       // of tiles kt .. kt + 3
-    const uint32_t to = lds0 + SCALES + (kt >> 2 & 1) * SBUF + wave * 256;
-    if (kt >= g.nk) return;
-    dma_word(rsa, scale_from, kt, to);
-    dma_word(rsb, scale_from, kt, to + BM * 4);
+  int round = 0;                                         // rounds of four steps in front of this tile
+  auto scale_at = [&](int kt) { return (round + (kt >> 2) & 1) * SBUF + (kt & 2); };   // of step kt and its neighbour
+  auto copy_scales = [&](int kt) {                       // of steps kt .. kt + 3
+    const uint32_t to = lds0 + SCALES + (round + (kt >> 2) & 1) * SBUF + wave * 256;
+    const bool in = kt < steps;
+    dma_word(rows_of(g.sa, in ? now.m0 : next.m0, g.M, BM, S, true), scale_from, in ? kt : 0, to);
+    dma_word(rows_of(g.sb, in ? now.n0 : next.n0, g.N, BN, S, true), scale_from, in ? kt : 0, to + BM * 4);
   };
-  floatx4 acc[8][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   const int r = lane & 15, q = lane >> 4;
   const int f0 = r * FB + 16 * (q ^ (r & 7)), f1 = r * FB + 16 * ((q + 4) ^ (r & 7));
   const char* const a0 = smem + wm * (64 * FB) + f0;     // fragment k of a set's A: + slot * SET + k * 16 * FB
@@ -469,7 +499,6 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
   const char* const b1 = smem + HALF + wn * (64 * FB) + f1;
   const char* const sca = smem + SCALES + wm * 512 + 4 * r;      // a fragment's scales: + 64 bytes each
   const char* const scb = smem + SCALES + BM * 4 + wn * 512 + 4 * r;
-  auto scale_at = [](int t) { return (t >> 2 & 1) * SBUF + (t & 2); };             // of tile t and its neighbour
   union Frag { intx8 v; u32x4 h[2]; };
   Frag fa[2], fb[2][8];
   int sa[2], sb[2][8];
@@ -479,15 +508,16 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
 
   copy_scales(0);
   aim(-1);
+  rb = rows_of(g.B, now.n0, g.N, BN, Kp, true);
 #pragma unroll
   for (int h = 0; h < 2; ++h)                            // B(0): the second halves of sets -2 and -1
 #pragma unroll
-    for (int c = 4; c < 8; ++c) copy(-1, h, 2 + h, c);
+    for (int c = 4; c < 8; ++c) copy(h, 2 + h, c);
   aim(0);
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int c = 0; c < 8; ++c) copy(0, h, h, c);
+    for (int c = 0; c < 8; ++c) copy(h, h, c);
   asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
   lds_barrier();
 #pragma unroll
@@ -500,11 +530,9 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
   lds_barrier();
   aim(1);
 #pragma unroll
-  for (int c = 0; c < 8; ++c) copy(1, 0, 2, c);
+  for (int c = 0; c < 8; ++c) copy(0, 2, c);
   asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
   lds_barrier();
-#pragma unroll
-  for (int c = 0; c < 8; ++c) copy(1, 1, 3, c);
   fa[0].h[0] = *reinterpret_cast<const u32x4*>(a0);
   fa[0].h[1] = *reinterpret_cast<const u32x4*>(a1);
   sa[0] = *reinterpret_cast<const uint16_t*>(sca + scale_at(0));
@@ -513,11 +541,13 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
   sb[1][0] = *reinterpret_cast<const uint16_t*>(scb + scale_at(1));
   AXONN_AS_LOADED(sa[0]);
   AXONN_AS_LOADED(sb[1][0]);
-  __builtin_amdgcn_sched_barrier(0);
 
-  // tile kt = 2 * round + J: fragments of A in turn; what is read belongs to the next fragment, a tile later behind the last one
-  auto step = [&](auto parity, int kt) {
+  floatx4 acc[8][8];
+  // step kt, of parity J: fragments of A in turn; what is read belongs to the next fragment, a step later behind the last one.
+  // FINAL: the tile's last step, the copies of whose last group wait for the epilogue.
+  auto step = [&](auto parity, auto final, int kt) {
     constexpr int J = decltype(parity)::value;
+    constexpr bool FINAL = decltype(final)::value;
     const char* const sa_now = sca + scale_at(kt);
     const char* const sa_next = sca + scale_at(kt + 1);
     const char* const sb_now = scb + scale_at(kt + 1);
@@ -527,46 +557,72 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
       const bool last = i == 7, opens = (i & 3) == 3;
       const int h = opens ? (i >> 2) ^ 1 : i >> 2;        // half of the set that is read
       const int k = (i + 1) & 3, slot = (2 * J + (last ? 2 : h)) & 3;
-      const int nb = last ? J : J ^ 1;                    // the B fragment read belongs to the next tile, or the one behind it
+      const int nb = last ? J : J ^ 1;                    // the B fragment read belongs to the next step, or the one behind it
       if (opens) {
         asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
         lds_barrier();
         if (i == 3) aim(kt + 2);
-        if (i == 3 && (kt & 3) == 0) copy_scales(kt + 4);
+        if (J == 0 && i == 3 && (kt & 3) == 0) copy_scales(kt + 4);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         mfma_fp8_acc<J>(acc[i][j], fb[J][j].v, fa[i & 1].v, sb[J][j], sa[i & 1]);
-        if (j == 0) fa[(i + 1) & 1].h[0] = *reinterpret_cast<const u32x4*>(a0 + slot * SET + k * 16 * FB);
-        if (j == 1) fa[(i + 1) & 1].h[1] = *reinterpret_cast<const u32x4*>(a1 + slot * SET + k * 16 * FB);
-        if (j == 2) sa[(i + 1) & 1] = *reinterpret_cast<const uint16_t*>((last ? sa_next : sa_now) + ((i + 1) & 7) * 64);
-        if (j == 3) sb[nb][4 * h + k] = *reinterpret_cast<const uint16_t*>((last ? sb_next : sb_now) + (4 * h + k) * 64);
-        if (j == 4) fb[nb][4 * h + k].h[0] = *reinterpret_cast<const u32x4*>(b0 + slot * SET + k * 16 * FB);
-        if (j == 5) fb[nb][4 * h + k].h[1] = *reinterpret_cast<const u32x4*>(b1 + slot * SET + k * 16 * FB);
+        if (j == 0) {
+          fa[(i + 1) & 1].h[0] = *reinterpret_cast<const u32x4*>(a0 + slot * SET + k * 16 * FB);
+          fa[(i + 1) & 1].h[1] = *reinterpret_cast<const u32x4*>(a1 + slot * SET + k * 16 * FB);
+        }
+        if (j == 1) {
+          sa[(i + 1) & 1] = *reinterpret_cast<const uint16_t*>((last ? sa_next : sa_now) + ((i + 1) & 7) * 64);
+          sb[nb][4 * h + k] = *reinterpret_cast<const uint16_t*>((last ? sb_next : sb_now) + (4 * h + k) * 64);
+        }
+        if (j == 2) fb[nb][4 * h + k].h[0] = *reinterpret_cast<const u32x4*>(b0 + slot * SET + k * 16 * FB);
+        if (j == 3) fb[nb][4 * h + k].h[1] = *reinterpret_cast<const u32x4*>(b1 + slot * SET + k * 16 * FB);
         if (j == 7) {
           AXONN_AS_LOADED(sa[(i + 1) & 1]);
           AXONN_AS_LOADED(sb[nb][4 * h + k]);
         }
-        if (opens) copy(kt + 2, i >> 2, (2 * J + (i >> 2)) & 3, j);
+        // two of a set's eight copies in each of the four groups from the one that opens: all at once they held the MFMAs up
+        if ((j == 4 || j == 6) && !(FINAL && last))
+          copy(i < 3 || last ? 1 : 0, (i < 3 ? 2 * J + 3 : last ? 2 * J + 1 : 2 * J) & 3, 2 * k + (j == 6));
         __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
-  // an odd number of tiles: one more, of zeros
-  int kt = 0;
-  do {
-    step(std::integral_constant<int, 0>{}, kt);
-    step(std::integral_constant<int, 1>{}, kt + 1);
-    kt += 2;
-  } while (kt < g.nk);
+  using std::integral_constant;
+  while (true) {
+    copy(1, 3, 0);                                       // what a tile's last group leaves to the next
+    copy(1, 3, 1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) asm volatile("" : "+a"(acc[i][j]));
+    asm volatile("s_nop 7");                             // behind them all: the compiler does not know that MFMAs read them
+    int kt = 0;
+    do {
+      step(integral_constant<int, 0>{}, integral_constant<bool, false>{}, kt);
+      step(integral_constant<int, 1>{}, integral_constant<bool, false>{}, kt + 1);
+      kt += 2;
+    } while (kt < steps - 2);
+    step(integral_constant<int, 0>{}, integral_constant<bool, false>{}, kt);
+    step(integral_constant<int, 1>{}, integral_constant<bool, true>{}, kt + 1);
+    // the matrix unit's last results; the compiler does not know what wrote them
+    asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+    fp8_epilogue<EPI, 8, 8, 1>(g, acc, (float*)(smem + 3 * SET) + wave * (16 * 128), now.m0 + wm * 128, now.n0 + wn * 128, lane);
+    pid += stride;
+    if (pid >= end) break;
+    lds_barrier();                                       // every wave is done with its part of the set
+    now = next;
+    next = tile_of(pid + stride);
+    round += steps >> 2;
+  }
+  dma_wait_all();                                        // copies past the end still write (zeros) to LDS
 #undef AXONN_AS_LOADED
-  // the matrix unit's last results; the compiler does not know what wrote them
-  asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-  dma_wait_all();                                        // copies of tiles past the end still write (zeros) to LDS
-  lds_barrier();
-  static_assert(4 * 64 * 132 * 4 <= (int)sizeof smem, "staging");
-  fp8_epilogue<EPI, 8, 8, 4>(g, acc, (float*)smem + wave * (64 * 132), m0 + wm * 128, n0 + wn * 128, lane);
 }
+
 template <int WM, int WN, int TM, int TN, int NS, int EPI>
 static hipError_t launch_fp8_tile(Fp8Args g, hipStream_t s) {
   constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
@@ -580,18 +636,34 @@ template <int EPI>
 static hipError_t launch_fp8_big(Fp8Args g, hipStream_t s) {
   g.tiles_m = (g.M + 255) / 256;
   g.tiles_n = (g.N + 255) / 256;
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_big_kernel<EPI>), dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(256), 0, s, g);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_big_kernel<EPI>), dim3((unsigned)std::min(256, g.tiles_m * g.tiles_n)), dim3(256), 0, s, g);
   return hipGetLastError();
 }
+// The kernel with the least modelled time: rounds of workgroups, each a fixed part and a part per 128 of k, in us.  The parts are
+// from single launches of outputs of 512 x 512 to 8192 x 20480 with K = 512 to 8192; a CU that is shared is slower per step.
+// Modelled / measured, 64 x 64, 128 x 128 and 256 x 256: 512 x 512 x 4096 8.8 / 8.8, 16.7 / 16.3, 43 / 42;  2048^3 16.4 / 15.7,
+// 11.1 / 12.1, 27 / 27;  2047 x 2048 x 8192 55 / 53, 37 / 38, 81 / 78;  2048 x 6144 x 2048 (two thirds of the CUs for the
+// last) 33 / 45, 33 / 34, 30 / 30;  4096^3 117 / 102, 80 / 78, 52 / 55.
 template <int EPI>
 static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
   auto tiles = [&](int64_t bm, int64_t bn) { return (g.M + bm - 1) / bm * ((g.N + bn - 1) / bn); };
-  if (tiles(256, 256) >= 256) {
-    if constexpr (EPI == EPI_ACC_F32) return launch_fp8_tile<2, 4, 4, 4, 2, EPI>(g, s);
-    else return launch_fp8_big<EPI>(g, s);
+  const int64_t t64 = tiles(64, 64), t128 = tiles(128, 128), t256 = tiles(256, 256);
+  auto rounds = [](int64_t t, int64_t per) { return (double)((t + per - 1) / per); };
+  if constexpr (EPI == EPI_ACC_F32) {
+    // bf16 MFMAs.  Modelled / measured, 64 x 64 and 128 x 128: 512 x 512 x 4096 14 / 14, 32 / 32;  2048^3 25 / 24, 24 / 24;
+    // 2047 x 2048 x 8192 86 / 82, 80 / 75;  2048 x 8192 x 2047 99 / 90, 73 / 73.
+    const double small = rounds(t64, 512) * (2.0 + g.nk * (t64 > 256 ? 0.64 : 0.39));
+    const double big = rounds(t128, 512) * (3.0 + g.nk * (t128 > 256 ? 2.1 : t128 > 128 ? 1.2 : 0.91));
+    if (small < big) return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
+    return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
+  } else {
+    const double small = rounds(t64, 512) * (1.8 + g.nk * (t64 > 256 ? 0.40 : 0.22));
+    const double mid = rounds(t128, 256) * (2.3 + g.nk * (t128 > 128 ? 0.55 : 0.45));
+    const double big = 4.0 + rounds(t256, 256) * (5.0 + (g.nk + 3) / 4 * 4 * (1.05 + 0.3 * std::min(1.0, t256 / 256.0)));
+    if (big < mid && big < small) return launch_fp8_big<EPI>(g, s);
+    if (mid < small) return launch_fp8_tile<2, 4, 4, 2, 4, EPI>(g, s);
+    return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
   }
-  if (tiles(128, 128) >= 192) return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
-  return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
 }
 
 hipError_t launch_gemm_fp8(int epi, int64_t M, int64_t N, int64_t K, const void* A, const void* a_scale, const void* B, const void* b_scale,
