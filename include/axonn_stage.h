@@ -557,7 +557,7 @@ int axonn_dropout_bwd(int64_t T, int64_t h, const void* dout_bf16, int64_t ld_do
  * behind K; scales [rows][4 * ceil(Kp / 512)], zeros behind the last block.
  * x [R, C]: q, scale receive its rows (blocks along C), q_t, scale_t the rows of its transpose
  * (C rows of R elements, blocks along R).  Either pair may be NULL; x is read once for both.
- * Codes 16-byte aligned, scales 4-byte aligned.  R, C <= 2^22. */
+ * Codes 16-byte aligned, scales 4-byte aligned.  R, C <= 2^22, R * C <= 2^36. */
 int axonn_fp8_quantize(int64_t R, int64_t C, const void* x_bf16, int64_t ld_x, void* q,
                        uint8_t* scale, void* q_t, uint8_t* scale_t, void* hip_stream);
 /* C[M,N] = epilogue( sum_k A(m,k) * B(n,k) ) of two matrices in that form (M and N rows of K

@@ -16,110 +16,193 @@ namespace axonn {
 constexpr int FB = 128;                      // elements of a block
 
 // ---------------------------------------------------------------------------------------------------------- quantiser
-// e of a block from its largest finite magnitude.
-__device__ __forceinline__ int block_exponent(float amax) {
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+#ifdef AXONN_ELEM_FP16
+typedef _Float16 elem_pair __attribute__((ext_vector_type(2)));
+#define AXONN_CVT_PK_FP8 __builtin_amdgcn_cvt_scalef32_pk_fp8_f16
+constexpr uint32_t kInfinity16 = 0x7c00;
+#else
+typedef __bf16 elem_pair __attribute__((ext_vector_type(2)));
+#define AXONN_CVT_PK_FP8 __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16
+constexpr uint32_t kInfinity16 = 0x7f80;
+#endif
+
+// Largest magnitude of both halves of a word and m's, as bit patterns (of non-negative numbers their order is the integers').
+__device__ __forceinline__ uint32_t max_magnitudes(uint32_t m, uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, w & 0x7fff7fffu)));
+}
+// The same without what is not finite.
+__device__ __forceinline__ uint32_t finite_magnitudes(uint32_t m, uint32_t w) {
+  w &= 0x7fff7fffu;
+  if ((w & 0xffffu) >= kInfinity16) w &= 0xffff0000u;
+  if ((w >> 16) >= kInfinity16) w &= 0xffffu;
+  return max_magnitudes(m, w);
+}
+// e of a block from the bit pattern of its largest finite magnitude.
+__device__ __forceinline__ int block_exponent(uint32_t pattern) {
+  const float amax = (float)__builtin_bit_cast(elem_t, (uint16_t)pattern);
   const uint32_t b = __float_as_uint(amax);
   return max(-127, (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0));       // 448 = 1.75 * 2^8
 }
-__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // -126 <= e <= 127
-__device__ __forceinline__ float finite_magnitude(float v) {
-  const float a = fabsf(v);
-  return a < INFINITY ? a : 0.f;             // an infinity or NaN has no part in the scale
+__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(e == -127 ? 0x400000u : (uint32_t)(e + 127) << 23); }   // -127 <= e <= 127
+// Codes of the four elements of two words, the first in the low byte: one rounding of x / scale to nearest, ties to even
+// (v_cvt_scalef32_pk_fp8_*, compared with the definition for every 16-bit pattern).
+__device__ __forceinline__ uint32_t encode4(uint32_t lo, uint32_t hi, float scale) {
+  s16x2 r = {0, 0};
+  r = AXONN_CVT_PK_FP8(r, __builtin_bit_cast(elem_pair, lo), scale, false);
+  r = AXONN_CVT_PK_FP8(r, __builtin_bit_cast(elem_pair, hi), scale, true);
+  return __builtin_bit_cast(uint32_t, r);
 }
-// Codes of four values, the first in the low byte; an infinity or NaN becomes 0x7f.
-__device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float inv) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
-  uint32_t bad = 0;
-  if (!(fabsf(a) < INFINITY)) bad |= 0x7fu;
-  if (!(fabsf(b) < INFINITY)) bad |= 0x7f00u;
-  if (!(fabsf(c) < INFINITY)) bad |= 0x7f0000u;
-  if (!(fabsf(d) < INFINITY)) bad |= 0x7f000000u;
-  return ((uint32_t)w | bad) & ~((bad & 0x40404040u) << 1);      // 0x7f, whatever the sign was
+// The same with 0x7f for every infinity and NaN.
+__device__ __forceinline__ uint32_t encode4_any(uint32_t lo, uint32_t hi, float scale) {
+  uint32_t c = encode4(lo, hi, scale);
+  if ((lo & 0x7fffu) >= kInfinity16) c = (c & 0xffffff00u) | 0x7fu;
+  if ((lo >> 16 & 0x7fffu) >= kInfinity16) c = (c & 0xffff00ffu) | 0x7f00u;
+  if ((hi & 0x7fffu) >= kInfinity16) c = (c & 0xff00ffffu) | 0x7f0000u;
+  if ((hi >> 16 & 0x7fffu) >= kInfinity16) c = (c & 0x00ffffffu) | 0x7f000000u;
+  return c;
 }
 
 struct QuantArgs {
   int R, C;                 // rows and columns of x
   const elem_t* x;
   int64_t ld_x;
-  uint8_t *q, *scale;       // [R][Cp], [R][S]         (null: not wanted)
+  uint8_t *q, *scale;       // [R][Cp], [R][S]
   uint8_t *q_t, *scale_t;   // [C][Rp], [C][S_t]
   int64_t Cp, S, Rp, S_t;
 };
 
-// One workgroup per block of 128 x 128 elements.  Read once; the rows' codes come straight from the registers, the columns'
-// through LDS: a thread owns two adjacent columns of a quarter of the rows.
-// Scale bytes behind the last block are cleared by the workgroup of that block.
+// The codes of a lane's chunk of 8 elements, one of the 16 lanes that share a block; e: the block's exponent.
+__device__ __forceinline__ u32x2 encode_chunk(u32x4 w, int& e) {
+  uint32_t m = max_magnitudes(max_magnitudes(max_magnitudes(w[0] & 0x7fff7fffu, w[1]), w[2]), w[3]);
+  m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  if (!__any(m >= kInfinity16)) {
+    e = block_exponent(m);
+    const float s = exp2_int(e);
+    return u32x2{encode4(w[0], w[1], s), encode4(w[2], w[3], s)};
+  }
+  m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = finite_magnitudes(m, w[i]);
+  m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+  e = block_exponent(m);
+  const float s = exp2_int(e);
+  return u32x2{encode4_any(w[0], w[1], s), encode4_any(w[2], w[3], s)};
+}
+
+// Rows alone: a wave takes 512 columns (four blocks, one word of scales) of ROWS rows.  HBM-bound.
+template <int ROWS>
+__global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(const QuantArgs g) {
+  const int lane = threadIdx.x & 63, quads = (int)(g.S / 4);
+  const int group = blockIdx.x / quads, quad = blockIdx.x - group * quads;
+  const int row0 = (group * 4 + (threadIdx.x >> 6)) * ROWS, c = quad * 512 + 8 * lane, n = g.C - c;
+  u32x4 w[ROWS];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    w[i] = u32x4{0, 0, 0, 0};
+    if (row0 + i < g.R && n > 0) w[i] = __builtin_bit_cast(u32x4, load_chunk(g.x + (int64_t)(row0 + i) * g.ld_x + c, n));
+  }
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    if (row0 + i >= g.R) return;
+    int e;
+    const u32x2 codes = encode_chunk(w[i], e);
+    if (c < g.Cp) *reinterpret_cast<u32x2*>(g.q + (int64_t)(row0 + i) * g.Cp + c) = codes;
+    // blocks behind the last hold zeros: byte 0
+    const uint32_t b = (uint32_t)(e + 127);
+    const uint32_t word = __builtin_amdgcn_readlane(b, 0) | __builtin_amdgcn_readlane(b, 16) << 8 | __builtin_amdgcn_readlane(b, 32) << 16 |
+                          __builtin_amdgcn_readlane(b, 48) << 24;
+    if (lane == 0) *reinterpret_cast<uint32_t*>(g.scale + (int64_t)(row0 + i) * g.S + 4 * quad) = word;
+  }
+}
+
+// The transpose, and with ROWS the rows too, of a block of 128 x 128 elements per workgroup, read once.  The rows' codes come
+// straight from the registers; the columns go through LDS: a thread has two adjacent columns (one word per row) of a quarter of
+// the rows.  Their codes lie in LDS with 16-byte chunk k of column c at k ^ (c / 2 % 8), without bank conflicts both ways.
+// Scale bytes behind the last block are cleared by the workgroup of that block.  HBM-bound.
 constexpr int QT_LD = FB + 8;                // elements of an LDS row
-template <bool ROWS, bool COLS>
-__global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantArgs g) {
-  __shared__ __align__(16) elem_t tile[COLS ? FB * QT_LD : 8];
-  __shared__ float col_max[COLS ? 4 : 1][FB];
-  __shared__ __align__(16) uint8_t codes_t[COLS ? FB * FB : 16];
-  const int tid = threadIdx.x, c0 = blockIdx.x * FB, r0 = blockIdx.y * FB;
-  const int ch = tid & 15, n = g.C - (c0 + 8 * ch);
+template <bool ROWS>
+__global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(const QuantArgs g) {
+  __shared__ __align__(16) char smem[FB * QT_LD * 2];
+  __shared__ uint32_t col_max[4][FB / 2];
+  elem_t* const tile = (elem_t*)smem;
+  const int tid = threadIdx.x;
+  const int blocks_c = (int)(g.Cp / FB), by = blockIdx.x / blocks_c, bx = blockIdx.x - by * blocks_c;
+  const int c0 = bx * FB, r0 = by * FB, ch = tid & 15, n = g.C - (c0 + 8 * ch);
+  u32x4 w[8];
+  const elem_t* const from = g.x + (int64_t)(r0 + (tid >> 4)) * g.ld_x + c0 + 8 * ch;
+  if (r0 + FB <= g.R && c0 + FB <= g.C) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const elemx8_any*>(from + (int64_t)(16 * i) * g.ld_x));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[i] = u32x4{0, 0, 0, 0};
+      if (r0 + 16 * i + (tid >> 4) < g.R && n > 0) w[i] = __builtin_bit_cast(u32x4, load_chunk(from + (int64_t)(16 * i) * g.ld_x, n));
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int r = i * 16 + (tid >> 4), row = r0 + r;
-    elemx8 v = {};
-    if (row < g.R && n > 0) v = load_chunk(g.x + (int64_t)row * g.ld_x + c0 + 8 * ch, n);
-    if (COLS) *reinterpret_cast<elemx8*>(tile + r * QT_LD + 8 * ch) = v;
+    const int r = 16 * i + (tid >> 4), row = r0 + r;
+    *reinterpret_cast<u32x4*>(tile + r * QT_LD + 8 * ch) = w[i];
     if (ROWS) {
-      float f[8], amax = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        f[e] = (float)v[e];
-        amax = fmaxf(amax, finite_magnitude(f[e]));
-      }
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o, 64));
-      const int ex = block_exponent(amax);
-      const float inv = exp2_int(-ex);
+      int e;
+      const u32x2 codes = encode_chunk(w[i], e);
       if (row < g.R) {
-        *reinterpret_cast<u32x2*>(g.q + (int64_t)row * g.Cp + c0 + 8 * ch) =
-            u32x2{encode4(f[0], f[1], f[2], f[3], inv), encode4(f[4], f[5], f[6], f[7], inv)};
-        const int last = (int)(g.Cp / FB) - 1, at = blockIdx.x;
-        if (ch == 0) g.scale[(int64_t)row * g.S + at] = (uint8_t)(ex + 127);
-        else if (at == last && at + ch < g.S) g.scale[(int64_t)row * g.S + at + ch] = 0;
+        *reinterpret_cast<u32x2*>(g.q + (int64_t)row * g.Cp + c0 + 8 * ch) = codes;
+        if (ch == 0) g.scale[(int64_t)row * g.S + bx] = (uint8_t)(e + 127);
+        else if (bx == blocks_c - 1 && bx + ch < g.S) g.scale[(int64_t)row * g.S + bx + ch] = 0;
       }
     }
   }
-  if (!COLS) return;
   __syncthreads();
   const int pair = tid & 63, quarter = tid >> 6;
-  float m0 = 0.f, m1 = 0.f;
-#pragma unroll 8
+  uint32_t v[32], m = 0;
+#pragma unroll
   for (int r = 0; r < 32; ++r) {
-    const elemx2 v = *reinterpret_cast<const elemx2*>(tile + (quarter * 32 + r) * QT_LD + 2 * pair);
-    m0 = fmaxf(m0, finite_magnitude((float)v[0]));
-    m1 = fmaxf(m1, finite_magnitude((float)v[1]));
+    v[r] = *reinterpret_cast<const uint32_t*>(tile + (quarter * 32 + r) * QT_LD + 2 * pair);
+    m = max_magnitudes(m, v[r]);
   }
-  col_max[quarter][2 * pair] = m0;
-  col_max[quarter][2 * pair + 1] = m1;
-  __syncthreads();
-  m0 = fmaxf(fmaxf(col_max[0][2 * pair], col_max[1][2 * pair]), fmaxf(col_max[2][2 * pair], col_max[3][2 * pair]));
-  m1 = fmaxf(fmaxf(col_max[0][2 * pair + 1], col_max[1][2 * pair + 1]), fmaxf(col_max[2][2 * pair + 1], col_max[3][2 * pair + 1]));
-  const int e0 = block_exponent(m0), e1 = block_exponent(m1);
-  const float i0 = exp2_int(-e0), i1 = exp2_int(-e1);
+  const bool odd_values = __syncthreads_or((m & 0xffffu) >= kInfinity16 || m >> 16 >= kInfinity16);
+  if (odd_values) {
+    m = 0;
 #pragma unroll
-  for (int r = 0; r < 32; r += 4) {
-    elemx2 v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = *reinterpret_cast<const elemx2*>(tile + (quarter * 32 + r + k) * QT_LD + 2 * pair);
-    *reinterpret_cast<uint32_t*>(codes_t + (2 * pair) * FB + quarter * 32 + r) =
-        encode4((float)v[0][0], (float)v[1][0], (float)v[2][0], (float)v[3][0], i0);
-    *reinterpret_cast<uint32_t*>(codes_t + (2 * pair + 1) * FB + quarter * 32 + r) =
-        encode4((float)v[0][1], (float)v[1][1], (float)v[2][1], (float)v[3][1], i1);
+    for (int r = 0; r < 32; ++r) m = finite_magnitudes(m, v[r]);
   }
-  const int last = (int)(g.Rp / FB) - 1, at = blockIdx.y;
+  col_max[quarter][pair] = m;
+  __syncthreads();                                       // everyone is done with the tile as well
+  m = max_magnitudes(max_magnitudes(max_magnitudes(col_max[0][pair], col_max[1][pair]), col_max[2][pair]), col_max[3][pair]);
+  const int e0 = block_exponent(m & 0xffffu), e1 = block_exponent(m >> 16);
+  const float s0 = exp2_int(e0), s1 = exp2_int(e1);
+  uint8_t* const codes_t = (uint8_t*)smem;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    u32x4 a, b;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t* x = v + 16 * k + 4 * j;
+      const uint32_t l0 = __builtin_amdgcn_perm(x[1], x[0], 0x05040100), l1 = __builtin_amdgcn_perm(x[3], x[2], 0x05040100);
+      const uint32_t h0 = __builtin_amdgcn_perm(x[1], x[0], 0x07060302), h1 = __builtin_amdgcn_perm(x[3], x[2], 0x07060302);
+      a[j] = odd_values ? encode4_any(l0, l1, s0) : encode4(l0, l1, s0);
+      b[j] = odd_values ? encode4_any(h0, h1, s1) : encode4(h0, h1, s1);
+    }
+    const int at = 16 * ((2 * quarter + k) ^ (pair & 7));
+    *reinterpret_cast<u32x4*>(codes_t + (2 * pair) * FB + at) = a;
+    *reinterpret_cast<u32x4*>(codes_t + (2 * pair + 1) * FB + at) = b;
+  }
   if (quarter == 0) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int col = c0 + 2 * pair + k;
       if (col >= g.C) continue;
-      g.scale_t[(int64_t)col * g.S_t + at] = (uint8_t)((k ? e1 : e0) + 127);
-      if (at == last)
-        for (int b = at + 1; b < g.S_t; ++b) g.scale_t[(int64_t)col * g.S_t + b] = 0;
+      g.scale_t[(int64_t)col * g.S_t + by] = (uint8_t)((k ? e1 : e0) + 127);
+      if (by == (int)(g.Rp / FB) - 1)
+        for (int b = by + 1; b < g.S_t; ++b) g.scale_t[(int64_t)col * g.S_t + b] = 0;
     }
   }
   __syncthreads();
@@ -128,7 +211,7 @@ __global__ __launch_bounds__(256) void fp8_quantize_kernel(const QuantArgs g) {
     const int col = i * 32 + (tid >> 3);
     if (c0 + col < g.C)
       *reinterpret_cast<u32x4*>(g.q_t + (int64_t)(c0 + col) * g.Rp + r0 + 16 * (tid & 7)) =
-          *reinterpret_cast<const u32x4*>(codes_t + col * FB + 16 * (tid & 7));
+          *reinterpret_cast<const u32x4*>(codes_t + col * FB + 16 * ((tid & 7) ^ (col >> 1 & 7)));
   }
 }
 
@@ -139,10 +222,18 @@ hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x
   g.q = (uint8_t*)q; g.scale = (uint8_t*)scale; g.q_t = (uint8_t*)q_t; g.scale_t = (uint8_t*)scale_t;
   g.Cp = (C + FB - 1) / FB * FB; g.Rp = (R + FB - 1) / FB * FB;
   g.S = (g.Cp / FB + 3) / 4 * 4; g.S_t = (g.Rp / FB + 3) / 4 * 4;
-  const dim3 grid((unsigned)(g.Cp / FB), (unsigned)(g.Rp / FB));
-  if (q && q_t) hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_kernel<true, true>), grid, dim3(256), 0, s, g);
-  else if (q) hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_kernel<true, false>), grid, dim3(256), 0, s, g);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_kernel<false, true>), grid, dim3(256), 0, s, g);
+  const unsigned tiles = (unsigned)(g.Cp / FB * (g.Rp / FB));
+  if (q_t) {
+    if (q) hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_tile_kernel<true>), dim3(tiles), dim3(256), 0, s, g);
+    else hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_tile_kernel<false>), dim3(tiles), dim3(256), 0, s, g);
+  } else {
+    // four rows in flight per lane where that leaves enough waves
+    const int64_t quads = g.S / 4;
+    if (R * quads >= 16384)
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_rows_kernel<4>), dim3((unsigned)((R + 15) / 16 * quads)), dim3(256), 0, s, g);
+    else
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_rows_kernel<1>), dim3((unsigned)((R + 3) / 4 * quads)), dim3(256), 0, s, g);
+  }
   return hipGetLastError();
 }
 

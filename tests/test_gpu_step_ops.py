@@ -288,6 +288,8 @@ def test_codes_and_scales(R, C, pad, shift):
         x[-2, ::3] = 3e38 if B.ELEM == "bf16" else 65504.0
         x[-3, 0], x[-4, C // 2] = np.inf, -np.inf
         x[-5, -1] = np.nan
+        x[-7] *= np.float32(2.0 ** -120 if B.ELEM == "bf16" else 2.0 ** -14)      # into the subnormal numbers
+        x[-8], x[-8, 3] = 0, 2.0 ** -133 if B.ELEM == "bf16" else 2.0 ** -24
     x = snap_elem(x).reshape(R, C)
     q, s, qt, st = quantised(x, ld=C + pad, shift=shift)
     for got, want in zip((q, s, qt, st), O.fp8_quantize(x) + O.fp8_quantize(x.T)):

@@ -107,6 +107,7 @@ def test_fp8():
     refused(INV, B.axonn_fp8_quantize, *with_args(ok, _5=A + 2))
     refused(INV, B.axonn_fp8_quantize, *with_args(ok, _0=0))
     refused(UNS, B.axonn_fp8_quantize, *with_args(ok, _0=(1 << 22) + 1))
+    refused(UNS, B.axonn_fp8_quantize, *with_args(ok, _0=1 << 22, _1=1 << 15, _3=1 << 15))
     ok = [0, 16, 16, 16, A, A, A, A, A, 16]
     for pos in (4, 5, 6, 7, 8):
         refused(INV, B.axonn_gemm_fp8, *with_args(ok, **{"_%d" % pos: None}))
