@@ -481,7 +481,7 @@ int axonn_adam_bucket(uint64_t n, float* theta, float* m, float* v, const void* 
  * ---------------------------------------------------------------------------------- */
 
 /* out[t,:] = scale * table[tokens[t],:], t < T; table [vocab, h] dense, out [T, h] with ld_out.
- * Ids outside [0, vocab) are clamped into range.  T <= 2^24, h <= 65535, vocab <= 2^30,
+ * Ids outside [0, vocab) are clamped into range.  T <= 2^24, h <= 65535, vocab <= 2^24,
  * vocab * h <= 2^34. */
 int axonn_embedding_fwd(int64_t T, int64_t h, int64_t vocab, const int32_t* tokens,
                         const void* table_bf16, float scale, void* out_bf16, int64_t ld_out,
@@ -557,7 +557,7 @@ int axonn_dropout_bwd(int64_t T, int64_t h, const void* dout_bf16, int64_t ld_do
  * behind K; scales [rows][4 * ceil(Kp / 512)], zeros behind the last block.
  * x [R, C]: q, scale receive its rows (blocks along C), q_t, scale_t the rows of its transpose
  * (C rows of R elements, blocks along R).  Either pair may be NULL; x is read once for both.
- * Codes 16-byte aligned, scales 4-byte aligned.  R, C <= 2^22, R * C <= 2^36. */
+ * Codes 16-byte aligned, scales 4-byte aligned.  R, C <= 2^22, R * C <= 2^35. */
 int axonn_fp8_quantize(int64_t R, int64_t C, const void* x_bf16, int64_t ld_x, void* q,
                        uint8_t* scale, void* q_t, uint8_t* scale_t, void* hip_stream);
 /* C[M,N] = epilogue( sum_k A(m,k) * B(n,k) ) of two matrices in that form (M and N rows of K

@@ -170,16 +170,109 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_scatter_kernel(co
   }
 }
 
+// Up to SORT_ONE_MAX tokens in one workgroup, in LDS, where id and token index together fit 32 bits; the other workgroups of the
+// launch clear the table meanwhile.  Each pass as in the scatter kernel above: a wave owns 64 * SORT_ONE_ITEMS consecutive places.
+constexpr int SORT_ONE_THREADS = 1024, SORT_ONE_WAVES = SORT_ONE_THREADS / 64, SORT_ONE_ITEMS = 16;
+constexpr int SORT_ONE_MAX = SORT_ONE_THREADS * SORT_ONE_ITEMS, SORT_ONE_BITS = 9;
+
+// Zeros to `halves` 16-bit numbers from p on, by workgroup `block` of `blocks`.
+template <int THREADS>
+__device__ __forceinline__ void clear_table(uint16_t* p, int64_t halves, int64_t block, int64_t blocks) {
+  for (int64_t i = (block * THREADS + threadIdx.x) * 8; i < halves; i += blocks * (THREADS * 8))
+    store_chunk((elem_t*)(p + i), elemx8{}, (int)min((int64_t)8, halves - i));
+}
+
+__global__ __launch_bounds__(SORT_ONE_THREADS) void embedding_sort_one_kernel(int T, int vocab, int bits, int t_bits, const int* __restrict__ tokens,
+                                                                              int* __restrict__ ids, int* __restrict__ order, uint16_t* clear,
+                                                                              int64_t halves) {
+  constexpr int BINS = 1 << SORT_ONE_BITS;
+  __shared__ uint32_t list[SORT_ONE_MAX];
+  __shared__ uint32_t counter[SORT_ONE_WAVES][BINS];
+  __shared__ uint32_t wave_total[BINS / 64];
+  if (blockIdx.x > 0) {
+    clear_table<SORT_ONE_THREADS>(clear, halves, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int items = (T + SORT_ONE_THREADS - 1) / SORT_ONE_THREADS, first = wave * 64 * items + lane;
+  uint32_t key[SORT_ONE_ITEMS], rank[SORT_ONE_ITEMS];
+#pragma unroll
+  for (int k = 0; k < SORT_ONE_ITEMS; ++k) {
+    const int i = first + 64 * k;
+    key[k] = k < items && i < T ? (uint32_t)clamp_token(tokens[i], vocab) << t_bits | (uint32_t)i : 0;
+  }
+  for (int shift = 0; shift < bits; shift += SORT_ONE_BITS) {
+    const int digit_bits = min(SORT_ONE_BITS, bits - shift), at = t_bits + shift;
+    for (int b = tid; b < SORT_ONE_WAVES * BINS; b += SORT_ONE_THREADS) (&counter[0][0])[b] = 0;
+    __syncthreads();
+    volatile uint32_t* const mine = counter[wave];
+#pragma unroll
+    for (int k = 0; k < SORT_ONE_ITEMS; ++k) {
+      const bool live = first + 64 * k < T;            // k < items where any lane is
+      if (k >= items) continue;
+      const uint32_t digit = key[k] >> at & ((1u << digit_bits) - 1);
+      unsigned long long peers = __ballot(live);
+      for (int bit = 0; bit < digit_bits; ++bit) {
+        const unsigned long long set = __ballot(digit >> bit & 1);
+        peers &= digit >> bit & 1 ? set : ~set;
+      }
+      const unsigned long long below = peers & ((1ull << lane) - 1);
+      const uint32_t old = live ? mine[digit] : 0;
+      rank[k] = old + __popcll(below);
+      __builtin_amdgcn_wave_barrier();                 // every lane has read before the first of a digit's lanes writes
+      if (live && below == 0) mine[digit] = old + __popcll(peers);
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // counters -> places: exclusive over the digits, then over the waves
+    uint32_t total = 0, scan = 0;
+    if (tid < BINS) {
+      for (int w = 0; w < SORT_ONE_WAVES; ++w) total += counter[w][tid];
+      scan = total;
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t up = __shfl_up(scan, o, 64);
+        if (lane >= o) scan += up;
+      }
+      if (lane == 63) wave_total[wave] = scan;
+    }
+    __syncthreads();
+    if (tid < BINS) {
+      uint32_t place = scan - total;
+      for (int w = 0; w < wave; ++w) place += wave_total[w];
+      for (int w = 0; w < SORT_ONE_WAVES; ++w) {
+        const uint32_t c = counter[w][tid];
+        counter[w][tid] = place;
+        place += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_ONE_ITEMS; ++k)
+      if (k < items && first + 64 * k < T) list[mine[key[k] >> at & ((1u << digit_bits) - 1)] + rank[k]] = key[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_ONE_ITEMS; ++k)
+      if (k < items && first + 64 * k < T) key[k] = list[first + 64 * k];
+  }
+#pragma unroll
+  for (int k = 0; k < SORT_ONE_ITEMS; ++k)
+    if (k < items && first + 64 * k < T) {
+      ids[first + 64 * k] = (int)(key[k] >> t_bits);
+      order[first + 64 * k] = (int)(key[k] & ((1u << t_bits) - 1));
+    }
+}
+
 // --------------------------------------------------------------------------------------------------------------- sums
-// The sorted list is cut into pieces of PIECE tokens; a wave adds the rows of one piece over 512 columns (8 per lane), a
-// batch of 8 rows in flight.  A run of equal ids that lies within the piece is finished here; one that crosses the piece's
-// start leaves its sum in partial[piece][0], one that begins in the piece and crosses its end in partial[piece][1], and
+// The sorted list is cut into pieces of PIECE tokens; a wave adds the rows of one piece over 512 columns (8 per lane), all
+// of them in flight.  A run of equal ids that lies within the piece is finished here; one that crosses the piece's start
+// leaves its sum in partial[piece][0], one that begins in the piece and crosses its end in partial[piece][1], and
 // embedding_bwd_join_kernel adds them up.
-constexpr int PIECE = 32, SUM_BATCH = 8, SUM_COLS = 512;
+constexpr int PIECE = 16, SUM_COLS = 512;
+typedef floatx4 floatx4_any __attribute__((aligned(4)));
 
 struct TableGrad {
   int T, h, vocab, pieces, col_chunks;
-  const int *ids, *order;            // sorted
+  const int *ids, *order;            // sorted (few tokens: ids are the tokens as they are)
   const elem_t* dout;
   int64_t ld_dout;
   float scale;
@@ -188,65 +281,97 @@ struct TableGrad {
   float* partial;                    // [pieces][2][h]
 };
 
+// Columns c .. c + n of row id, n of 8 (8 or more: all).
 template <bool FP32>
 __device__ __forceinline__ void store_table_row(const TableGrad& g, int id, int c, int n, const float (&acc)[8]) {
+  const float scale = g.scale;
+  const bool accumulate = g.accumulate;
   if constexpr (FP32) {
     float* p = (float*)g.dtable + (int64_t)id * g.h + c;
+    if (n >= 8) {
+      floatx4_any* const v = (floatx4_any*)p;
+      floatx4 lo = {acc[0], acc[1], acc[2], acc[3]}, hi = {acc[4], acc[5], acc[6], acc[7]};
+      lo *= scale;
+      hi *= scale;
+      if (accumulate) { lo += v[0]; hi += v[1]; }
+      v[0] = lo;
+      v[1] = hi;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) p[e] = acc[e] * g.scale + (g.accumulate ? p[e] : 0.f);
+      for (int e = 0; e < 7; ++e)
+        if (e < n) p[e] = acc[e] * scale + (accumulate ? p[e] : 0.f);
+    }
   } else {
     elem_t* p = (elem_t*)g.dtable + (int64_t)id * g.h + c;
     elemx8 o, old = {};
-    if (g.accumulate) old = load_chunk(p, n);
+    if (accumulate) old = load_chunk(p, n);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = (elem_t)(acc[e] * g.scale + (float)old[e]);
+    for (int e = 0; e < 8; ++e) o[e] = (elem_t)(acc[e] * scale + (float)old[e]);
     store_chunk(p, o, n);
   }
+}
+__device__ __forceinline__ void add_chunk(float (&acc)[8], const elemx8& v) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] += (float)v[e];
 }
 
 template <bool FP32>
 __global__ __launch_bounds__(256) void embedding_bwd_sum_kernel(const TableGrad g) {
   const int lane = threadIdx.x & 63;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int piece = (int)(w / g.col_chunks), c = (int)(w - (int64_t)piece * g.col_chunks) * SUM_COLS + 8 * lane, n = g.h - c;
   if (piece >= g.pieces) return;
   const int first = piece * PIECE, count = min(PIECE, g.T - first);
-  const int id = lane < count ? g.ids[first + lane] : -1, row = lane < count ? g.order[first + lane] : 0;
+  const int mine = first + min(lane, count - 1);
+  const int lane_id = g.ids[mine], lane_row = g.order[mine];
   const int before = first > 0 ? g.ids[first - 1] : -1, behind = first + count < g.T ? g.ids[first + count] : -1;
+  // Ids and rows as scalars, in front of every branch that lanes take differently: in such a branch the registers of lanes that
+  // are not in it may hold anything.  Places past the last token repeat it, and are not added.
+  int id[PIECE + 1], row[PIECE];
+#pragma unroll
+  for (int k = 0; k < PIECE; ++k) {
+    id[k] = __builtin_amdgcn_readlane(lane_id, k);
+    row[k] = __builtin_amdgcn_readlane(lane_row, k);
+  }
+  id[PIECE] = behind;
+  elemx8 v[PIECE];
+  if (n >= 8) {
+#pragma unroll
+    for (int k = 0; k < PIECE; ++k) v[k] = *reinterpret_cast<const elemx8_any*>(g.dout + (int64_t)row[k] * g.ld_dout + c);
+  } else if (n > 0) {
+    // the lane of the last, shorter chunk, element by element
+#pragma unroll
+    for (int k = 0; k < PIECE; ++k) v[k] = load_chunk(g.dout + (int64_t)row[k] * g.ld_dout + c, n);
+  }
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
   bool from_start = true;                               // the run at hand began with the piece
-  for (int i0 = 0; i0 < count; i0 += SUM_BATCH) {
-    elemx8 v[SUM_BATCH];
 #pragma unroll
-    for (int k = 0; k < SUM_BATCH; ++k) {
-      const int r = __builtin_amdgcn_readlane(row, min(i0 + k, count - 1));
-      if (n > 0) v[k] = load_chunk(g.dout + (int64_t)r * g.ld_dout + c, n);
-    }
+  for (int i = 0; i < PIECE; ++i) {
+    if (i < count) {
+      const int cur = id[i], next = i + 1 < count ? id[i + 1] : behind;
+      add_chunk(acc, v[i]);
+      if (next != cur || i + 1 == count) {
+        const bool head = from_start && before == cur, tail = next == cur;
+        if (n > 0) {
+          if (!head && !tail) store_table_row<FP32>(g, cur, c, n, acc);
+          else {
+            float* p = g.partial + ((int64_t)piece * 2 + (head ? 0 : 1)) * g.h + c;
+            if (n >= 8) {
+              ((floatx4_any*)p)[0] = floatx4{acc[0], acc[1], acc[2], acc[3]};
+              ((floatx4_any*)p)[1] = floatx4{acc[4], acc[5], acc[6], acc[7]};
+            } else {
 #pragma unroll
-    for (int k = 0; k < SUM_BATCH; ++k) {
-      const int i = i0 + k;
-      if (i >= count) break;
-      const int cur = __builtin_amdgcn_readlane(id, i);
-      const int next = i + 1 < count ? __builtin_amdgcn_readlane(id, min(i + 1, 63)) : behind;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += (float)v[k][e];
-      if (next == cur && i + 1 < count) continue;
-      const bool head = from_start && before == cur, tail = next == cur;
-      if (n > 0) {
-        if (!head && !tail) store_table_row<FP32>(g, cur, c, n, acc);
-        else {
-          float* p = g.partial + ((int64_t)piece * 2 + (head ? 0 : 1)) * g.h + c;
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = acc[e];
+              for (int e = 0; e < 7; ++e)
+                if (e < n) p[e] = acc[e];
+            }
+          }
         }
-      }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-      from_start = false;
+        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+        from_start = false;
+      }
     }
   }
 }
@@ -256,31 +381,53 @@ __global__ __launch_bounds__(256) void embedding_bwd_sum_kernel(const TableGrad 
 template <bool FP32>
 __global__ __launch_bounds__(256) void embedding_bwd_join_kernel(const TableGrad g) {
   __shared__ float sums[3][64][8];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = blockIdx.x;
   const int c = blockIdx.y * SUM_COLS + 8 * lane, n = g.h - c;
   const int first = piece * PIECE, last = first + PIECE - 1;
   if (last + 1 >= g.T) return;
   const int id = g.ids[last];
   if (g.ids[last + 1] != id || (first > 0 && g.ids[first - 1] == id && g.ids[first] == id)) return;
-  // the last piece that begins with this id: ids at the pieces' starts are sorted
-  int lo = piece + 1, hi = g.pieces - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (g.ids[mid * PIECE] == id) lo = mid;
-    else hi = mid - 1;
+  // pieces that begin with this id, 64 at a time
+  int parts = 1;                                        // partial[piece][1], then partial[piece + 1 ..][0]
+  for (int p = piece + 1;; p += 64) {
+    const unsigned long long same = __ballot(p + lane < g.pieces && g.ids[min(p + lane, g.pieces - 1) * PIECE] == id);
+    parts += ~same ? __ffsll(~same) - 1 : 64;
+    if (~same) break;
   }
-  const int parts = lo - piece + 1;                     // partial[piece][1], then partial[piece + 1 .. lo][0]
   const int share = (parts + 3) / 4, p0 = wave * share, p1 = min(parts, p0 + share);
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-  if (n > 0)
-    for (int q = p0; q < p1; ++q) {
-      const float* p = g.partial + ((int64_t)(piece + q) * 2 + (q == 0 ? 1 : 0)) * g.h + c;
+  auto part = [&](int q) { return g.partial + ((int64_t)(piece + q) * 2 + (q == 0 ? 1 : 0)) * g.h + c; };
+  if (n >= 8) {
+    int q = p0;
+    for (; q + 8 <= p1; q += 8) {
+      floatx4 v[8][2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int k = 0; k < 8; ++k) {
+        const floatx4_any* const p = (const floatx4_any*)part(q + k);
+        v[k][0] = p[0];
+        v[k][1] = p[1];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += v[k][e >> 2][e & 3];
+    }
+    for (; q < p1; ++q) {
+      const floatx4_any* const p = (const floatx4_any*)part(q);
+      const floatx4 lo = p[0], hi = p[1];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += e < 4 ? lo[e] : hi[e - 4];
+    }
+  } else if (n > 0) {
+    for (int q = p0; q < p1; ++q) {
+      const float* const p = part(q);
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
         if (e < n) acc[e] += p[e];
     }
+  }
   if (wave > 0) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sums[wave - 1][lane][e] = acc[e];
@@ -294,10 +441,99 @@ __global__ __launch_bounds__(256) void embedding_bwd_join_kernel(const TableGrad
   store_table_row<FP32>(g, id, c, n, acc);
 }
 
-// bytes of zeros at p (any 2-byte aligned address).
+// Up to FEW_MAX tokens: no sort, one launch, every row of the result has one writer.  A workgroup takes ROWS rows of the table
+// (accumulating: the ids of ROWS tokens, those that no earlier token has) and 512 columns, marks in bit masks which tokens
+// name them, and its waves add the marked rows of dout in token order, eight in flight; the tokens of a row with many are
+// shared out to the four waves.  Rows without tokens are cleared.
+constexpr int FEW_MAX = 1024, FEW_SHARED = 32;
+template <bool FP32, int ROWS>
+__global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const TableGrad g) {
+  __shared__ unsigned long long mask[ROWS][FEW_MAX / 64];
+  __shared__ float sums[3][64][8];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r0 = blockIdx.x * ROWS, c = blockIdx.y * SUM_COLS + 8 * lane, n = g.h - c, words = (g.T + 63) / 64;
+  auto row_id = [&](int r) {                            // -1: none
+    const int i = r0 + r;
+    if (g.accumulate) return i < g.T ? clamp_token(g.ids[i], g.vocab) : -1;
+    return i < g.vocab ? i : -1;
+  };
+  int want[ROWS];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) want[r] = row_id(r);
+  for (int w = wave; w < words; w += 4) {
+    const int t = w * 64 + lane, id = t < g.T ? clamp_token(g.ids[t], g.vocab) : -2;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      const unsigned long long m = __ballot(id == want[r]);
+      if (lane == 0) mask[r][w] = m;
+    }
+  }
+  __syncthreads();
+  // adds the tokens marked in words [w0, w1)
+  auto add = [&](int r, int w0, int w1, float (&acc)[8]) {
+    int rows[8], k = 0;
+    auto flush = [&]() {
+      elemx8 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < k && n > 0) v[i] = load_chunk(g.dout + (int64_t)rows[i] * g.ld_dout + c, n);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < k) add_chunk(acc, v[i]);
+      k = 0;
+    };
+    for (int w = w0; w < w1; ++w) {
+      unsigned long long m = mask[r][w];
+      m = (unsigned long long)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
+      while (m) {
+        const int t = w * 64 + __ffsll(m) - 1;
+        m &= m - 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i == k) rows[i] = t;
+        if (++k == 8) flush();
+      }
+    }
+    if (k) flush();
+  };
+#pragma unroll 1
+  for (int r = 0; r < ROWS; ++r) {
+    const int id = row_id(r);
+    if (id < 0) break;
+    int tokens = 0, earlier = 0;
+    for (int w = 0; w < words; ++w) {
+      const unsigned long long m = mask[r][w];
+      tokens += __popcll(m);
+      if (g.accumulate && w * 64 < r0 + r) earlier |= (w * 64 + 64 <= r0 + r ? m : m & ((1ull << ((r0 + r) & 63)) - 1)) != 0;
+    }
+    if (earlier) continue;
+    const bool shared = tokens > FEW_SHARED;            // the same for the whole workgroup
+    if (!shared && (r & 3) != wave) continue;
+    float acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    if (!shared) add(r, 0, words, acc);
+    else {
+      const int part = (words + 3) / 4;
+      add(r, min(words, wave * part), min(words, (wave + 1) * part), acc);
+      __syncthreads();
+      if (wave > 0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[wave - 1][lane][e] = acc[e];
+      }
+      __syncthreads();
+      if (wave > 0) continue;
+#pragma unroll
+      for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += sums[w][lane][e];
+    }
+    if (n > 0) store_table_row<FP32>(g, id, c, n, acc);
+  }
+}
+
 __global__ __launch_bounds__(256) void embedding_clear_kernel(uint16_t* p, int64_t halves) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-  if (i < halves) store_chunk((elem_t*)(p + i), elemx8{}, (int)min((int64_t)8, halves - i));
+  clear_table<256>(p, halves, blockIdx.x, gridDim.x);
 }
 
 // Workspace, in this order, each part at a multiple of 256 bytes.
@@ -306,64 +542,84 @@ struct EmbeddingWs {
   uint64_t keys[2], index[2], hist, partial, bytes;
 };
 static EmbeddingWs embedding_ws(int64_t T, int64_t h, int64_t vocab) {
-  EmbeddingWs w;
+  EmbeddingWs w = {};
   w.bits = 1;
   while (((int64_t)1 << w.bits) < vocab) ++w.bits;
-  const int64_t tiles = (T + SORT_TILE - 1) / SORT_TILE;
-  const int64_t per = (tiles + SORT_MAX_BLOCKS - 1) / SORT_MAX_BLOCKS;
-  w.per_block = (int)(per * SORT_TILE);
-  w.blocks = (int)((tiles + per - 1) / per);
-  w.pieces = (int)((T + PIECE - 1) / PIECE);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) { const uint64_t r = at; at += (bytes + 255) / 256 * 256; return r; };
-  for (int i = 0; i < 2; ++i) { w.keys[i] = take(4 * (uint64_t)T); w.index[i] = take(4 * (uint64_t)T); }
-  w.hist = take(4ull * w.blocks << SORT_MAX_BITS);
-  w.partial = take(8ull * w.pieces * (uint64_t)h);
-  w.bytes = at;
+  if (T > FEW_MAX) {
+    const int64_t tiles = (T + SORT_TILE - 1) / SORT_TILE;
+    const int64_t per = (tiles + SORT_MAX_BLOCKS - 1) / SORT_MAX_BLOCKS;
+    w.per_block = (int)(per * SORT_TILE);
+    w.blocks = (int)((tiles + per - 1) / per);
+    w.pieces = (int)((T + PIECE - 1) / PIECE);
+    for (int i = 0; i < 2; ++i) { w.keys[i] = take(4 * (uint64_t)T); w.index[i] = take(4 * (uint64_t)T); }
+    w.hist = take(4ull * w.blocks << SORT_MAX_BITS);
+    w.partial = take(8ull * w.pieces * (uint64_t)h);
+  }
+  w.bytes = std::max<uint64_t>(at, 16);
   return w;
 }
 uint64_t embedding_bwd_ws_bytes(int64_t T, int64_t h, int64_t vocab) { return embedding_ws(T, h, vocab).bytes; }
 
+template <bool FP32>
+static hipError_t launch_embedding_bwd_t(TableGrad g, const EmbeddingWs& w, const int* tokens, char* ws, hipStream_t s) {
+  const int64_t T = g.T, halves = (int64_t)g.vocab * g.h * (FP32 ? 2 : 1);
+  if (T <= FEW_MAX) {
+    g.ids = tokens;
+    const int64_t rows = g.accumulate ? T : g.vocab;
+    // more rows per workgroup where there are workgroups enough: each looks at every token once
+    if (rows > 8192)
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_few_kernel<FP32, 16>), dim3((unsigned)((rows + 15) / 16), g.col_chunks), dim3(256), 0, s, g);
+    else
+      hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_few_kernel<FP32, 4>), dim3((unsigned)((rows + 3) / 4), g.col_chunks), dim3(256), 0, s, g);
+    return hipGetLastError();
+  }
+  int t_bits = 1;
+  while (((int64_t)1 << t_bits) < T) ++t_bits;
+  if (T <= SORT_ONE_MAX && w.bits + t_bits <= 32) {
+    // a workgroup of the clearing part has 16 KB at least
+    const int64_t clearing = g.accumulate ? 0 : std::min<int64_t>(1024, (halves + 8191) / 8192);
+    hipLaunchKernelGGL(embedding_sort_one_kernel, dim3((unsigned)(1 + clearing)), dim3(SORT_ONE_THREADS), 0, s, g.T, g.vocab, w.bits, t_bits, tokens,
+                       (int*)(ws + w.keys[0]), (int*)(ws + w.index[0]), (uint16_t*)g.dtable, halves);
+    g.ids = (const int*)(ws + w.keys[0]); g.order = (const int*)(ws + w.index[0]);
+  } else {
+    if (!g.accumulate)
+      hipLaunchKernelGGL(embedding_clear_kernel, dim3((unsigned)std::min<int64_t>(4096, (halves + 2047) / 2048)), dim3(256), 0, s,
+                         (uint16_t*)g.dtable, halves);
+    const int passes = (w.bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS;
+    for (int i = 0, shift = 0; i < passes; ++i) {
+      SortPass p;
+      p.T = g.T; p.per_block = w.per_block; p.vocab = g.vocab;
+      p.bits = (w.bits - shift + passes - i - 1) / (passes - i);
+      p.shift = shift;
+      const int to = i & 1, from = to ^ 1;
+      p.keys_in = i == 0 ? tokens : (const int*)(ws + w.keys[from]);
+      p.index_in = i == 0 ? nullptr : (const int*)(ws + w.index[from]);
+      p.keys_out = (int*)(ws + w.keys[to]); p.index_out = (int*)(ws + w.index[to]);
+      p.hist = (uint32_t*)(ws + w.hist);
+      const int bins = 1 << p.bits;
+      hipLaunchKernelGGL(embedding_sort_hist_kernel, dim3(w.blocks), dim3(SORT_THREADS), bins * 4, s, p);
+      hipLaunchKernelGGL(embedding_sort_scatter_kernel, dim3(w.blocks), dim3(SORT_THREADS), ((SORT_WAVES + 1) * bins + SORT_WAVES) * 4, s, p,
+                         w.blocks);
+      shift += p.bits;
+    }
+    g.ids = (const int*)(ws + w.keys[(passes - 1) & 1]); g.order = (const int*)(ws + w.index[(passes - 1) & 1]);
+  }
+  g.partial = (float*)(ws + w.partial);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_sum_kernel<FP32>), dim3((unsigned)(((int64_t)g.pieces * g.col_chunks + 3) / 4)), dim3(256), 0,
+                     s, g);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_join_kernel<FP32>), dim3(g.pieces, g.col_chunks), dim3(256), 0, s, g);
+  return hipGetLastError();
+}
+
 hipError_t launch_embedding_bwd(int64_t T, int64_t h, int64_t vocab, const int* tokens, const void* dout, int64_t ld_dout, float scale,
                                 void* dtable, bool fp32, bool accumulate, void* workspace, hipStream_t s) {
   const EmbeddingWs w = embedding_ws(T, h, vocab);
-  char* const ws = (char*)workspace;
-  if (!accumulate) {
-    const int64_t halves = vocab * h * (fp32 ? 2 : 1);
-    hipLaunchKernelGGL(embedding_clear_kernel, dim3((unsigned)((halves + 2047) / 2048)), dim3(256), 0, s, (uint16_t*)dtable, halves);
-  }
-  const int passes = (w.bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS;
-  for (int i = 0, shift = 0; i < passes; ++i) {
-    SortPass p;
-    p.T = (int)T; p.per_block = w.per_block; p.vocab = (int)vocab;
-    p.bits = (w.bits - shift + passes - i - 1) / (passes - i);
-    p.shift = shift;
-    const int to = i & 1, from = to ^ 1;
-    p.keys_in = i == 0 ? tokens : (const int*)(ws + w.keys[from]);
-    p.index_in = i == 0 ? nullptr : (const int*)(ws + w.index[from]);
-    p.keys_out = (int*)(ws + w.keys[to]); p.index_out = (int*)(ws + w.index[to]);
-    p.hist = (uint32_t*)(ws + w.hist);
-    const int bins = 1 << p.bits;
-    hipLaunchKernelGGL(embedding_sort_hist_kernel, dim3(w.blocks), dim3(SORT_THREADS), bins * 4, s, p);
-    hipLaunchKernelGGL(embedding_sort_scatter_kernel, dim3(w.blocks), dim3(SORT_THREADS), ((SORT_WAVES + 1) * bins + SORT_WAVES) * 4, s, p,
-                       w.blocks);
-    shift += p.bits;
-  }
-  TableGrad g;
+  TableGrad g = {};
   g.T = (int)T; g.h = (int)h; g.vocab = (int)vocab; g.pieces = w.pieces; g.col_chunks = (int)((h + SUM_COLS - 1) / SUM_COLS);
-  g.ids = (const int*)(ws + w.keys[(passes - 1) & 1]); g.order = (const int*)(ws + w.index[(passes - 1) & 1]);
   g.dout = (const elem_t*)dout; g.ld_dout = ld_dout; g.scale = scale; g.accumulate = accumulate; g.dtable = dtable;
-  g.partial = (float*)(ws + w.partial);
-  const unsigned blocks = (unsigned)(((int64_t)g.pieces * g.col_chunks + 3) / 4);
-  const dim3 join(g.pieces, g.col_chunks);
-  if (fp32) {
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_sum_kernel<true>), dim3(blocks), dim3(256), 0, s, g);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_join_kernel<true>), join, dim3(256), 0, s, g);
-  } else {
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_sum_kernel<false>), dim3(blocks), dim3(256), 0, s, g);
-    hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_join_kernel<false>), join, dim3(256), 0, s, g);
-  }
-  return hipGetLastError();
+  return fp32 ? launch_embedding_bwd_t<true>(g, w, tokens, (char*)workspace, s) : launch_embedding_bwd_t<false>(g, w, tokens, (char*)workspace, s);
 }
 
 }  // namespace axonn

@@ -54,9 +54,8 @@ __device__ __forceinline__ uint32_t encode4(uint32_t lo, uint32_t hi, float scal
   r = AXONN_CVT_PK_FP8(r, __builtin_bit_cast(elem_pair, hi), scale, true);
   return __builtin_bit_cast(uint32_t, r);
 }
-// The same with 0x7f for every infinity and NaN.
-__device__ __forceinline__ uint32_t encode4_any(uint32_t lo, uint32_t hi, float scale) {
-  uint32_t c = encode4(lo, hi, scale);
+// Puts 0x7f in the codes `c` of the infinities and NaN among the four elements.
+__device__ __forceinline__ uint32_t mark_not_finite(uint32_t c, uint32_t lo, uint32_t hi) {
   if ((lo & 0x7fffu) >= kInfinity16) c = (c & 0xffffff00u) | 0x7fu;
   if ((lo >> 16 & 0x7fffu) >= kInfinity16) c = (c & 0xffff00ffu) | 0x7f00u;
   if ((hi & 0x7fffu) >= kInfinity16) c = (c & 0xff00ffffu) | 0x7f0000u;
@@ -92,31 +91,33 @@ __device__ __forceinline__ u32x2 encode_chunk(u32x4 w, int& e) {
   for (int o = 8; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
   e = block_exponent(m);
   const float s = exp2_int(e);
-  return u32x2{encode4_any(w[0], w[1], s), encode4_any(w[2], w[3], s)};
+  return u32x2{mark_not_finite(encode4(w[0], w[1], s), w[0], w[1]), mark_not_finite(encode4(w[2], w[3], s), w[2], w[3])};
 }
 
-// Rows alone: a wave takes 512 columns (four blocks, one word of scales) of ROWS rows.  HBM-bound.
-template <int ROWS>
+// Rows alone: a wave takes 512 columns (four blocks, one word of scales) of QR_ROWS rows.  HBM-bound: 8192 x 5120 in 21.4 us
+// (5.9 TB/s), 8192 x 20480 83 (6.0), 2047 x 8192 10.5, 200 x 392 4.5 by launches one behind the other; 1, 4 and 8 rows per wave
+// 23.5, 22.2, 24.0 for the first, 4.7, 5.3, 4.9 for the last.
+constexpr int QR_ROWS = 2;
 __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(const QuantArgs g) {
   const int lane = threadIdx.x & 63, quads = (int)(g.S / 4);
   const int group = blockIdx.x / quads, quad = blockIdx.x - group * quads;
-  const int row0 = (group * 4 + (threadIdx.x >> 6)) * ROWS, c = quad * 512 + 8 * lane, n = g.C - c;
-  u32x4 w[ROWS];
+  const int row0 = (group * 4 + (threadIdx.x >> 6)) * QR_ROWS, c = quad * 512 + 8 * lane, n = g.C - c;
+  u32x4 w[QR_ROWS];
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
+  for (int i = 0; i < QR_ROWS; ++i) {
     w[i] = u32x4{0, 0, 0, 0};
     if (row0 + i < g.R && n > 0) w[i] = __builtin_bit_cast(u32x4, load_chunk(g.x + (int64_t)(row0 + i) * g.ld_x + c, n));
   }
 #pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
+  for (int i = 0; i < QR_ROWS; ++i) {
     if (row0 + i >= g.R) return;
     int e;
     const u32x2 codes = encode_chunk(w[i], e);
-    if (c < g.Cp) *reinterpret_cast<u32x2*>(g.q + (int64_t)(row0 + i) * g.Cp + c) = codes;
     // blocks behind the last hold zeros: byte 0
     const uint32_t b = (uint32_t)(e + 127);
     const uint32_t word = __builtin_amdgcn_readlane(b, 0) | __builtin_amdgcn_readlane(b, 16) << 8 | __builtin_amdgcn_readlane(b, 32) << 16 |
                           __builtin_amdgcn_readlane(b, 48) << 24;
+    if (c < g.Cp) *reinterpret_cast<u32x2*>(g.q + (int64_t)(row0 + i) * g.Cp + c) = codes;
     if (lane == 0) *reinterpret_cast<uint32_t*>(g.scale + (int64_t)(row0 + i) * g.S + 4 * quad) = word;
   }
 }
@@ -124,10 +125,11 @@ __global__ __launch_bounds__(256) void fp8_quantize_rows_kernel(const QuantArgs 
 // The transpose, and with ROWS the rows too, of a block of 128 x 128 elements per workgroup, read once.  The rows' codes come
 // straight from the registers; the columns go through LDS: a thread has two adjacent columns (one word per row) of a quarter of
 // the rows.  Their codes lie in LDS with 16-byte chunk k of column c at k ^ (c / 2 % 8), without bank conflicts both ways.
-// Scale bytes behind the last block are cleared by the workgroup of that block.  HBM-bound.
+// Scale bytes behind the last block are cleared by the workgroup of that block.  HBM-bound: 16384 x 5120 in 71 us (4.7 TB/s)
+// with the rows, 47 (5.3) without; 2047 x 8192 17.7 and 12.4.
 constexpr int QT_LD = FB + 8;                // elements of an LDS row
 template <bool ROWS>
-__global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(const QuantArgs g) {
+__global__ __launch_bounds__(256, 4) void fp8_quantize_tile_kernel(const QuantArgs g) {
   __shared__ __align__(16) char smem[FB * QT_LD * 2];
   __shared__ uint32_t col_max[4][FB / 2];
   elem_t* const tile = (elem_t*)smem;
@@ -136,20 +138,26 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(const QuantArgs 
   const int c0 = bx * FB, r0 = by * FB, ch = tid & 15, n = g.C - (c0 + 8 * ch);
   u32x4 w[8];
   const elem_t* const from = g.x + (int64_t)(r0 + (tid >> 4)) * g.ld_x + c0 + 8 * ch;
+  elem_t* const mine = tile + (tid >> 4) * QT_LD + 8 * ch;
   if (r0 + FB <= g.R && c0 + FB <= g.C) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = __builtin_bit_cast(u32x4, *reinterpret_cast<const elemx8_any*>(from + (int64_t)(16 * i) * g.ld_x));
-  } else {
 #pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(mine + 16 * i * QT_LD) = w[i];
+  } else {
+    // at the edges chunk by chunk: element-wise loads of all eight at once take more registers than there are
+#pragma unroll 1
     for (int i = 0; i < 8; ++i) {
-      w[i] = u32x4{0, 0, 0, 0};
-      if (r0 + 16 * i + (tid >> 4) < g.R && n > 0) w[i] = __builtin_bit_cast(u32x4, load_chunk(from + (int64_t)(16 * i) * g.ld_x, n));
+      elemx8 v = {};
+      if (r0 + 16 * i + (tid >> 4) < g.R && n > 0) v = load_chunk(from + (int64_t)(16 * i) * g.ld_x, n);
+      *reinterpret_cast<elemx8*>(mine + 16 * i * QT_LD) = v;
     }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const u32x4*>(mine + 16 * i * QT_LD);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int r = 16 * i + (tid >> 4), row = r0 + r;
-    *reinterpret_cast<u32x4*>(tile + r * QT_LD + 8 * ch) = w[i];
+    const int row = r0 + 16 * i + (tid >> 4);
     if (ROWS) {
       int e;
       const u32x2 codes = encode_chunk(w[i], e);
@@ -180,16 +188,22 @@ __global__ __launch_bounds__(256) void fp8_quantize_tile_kernel(const QuantArgs 
   const int e0 = block_exponent(m & 0xffffu), e1 = block_exponent(m >> 16);
   const float s0 = exp2_int(e0), s1 = exp2_int(e1);
   uint8_t* const codes_t = (uint8_t*)smem;
+  auto low = [&](int i) { return __builtin_amdgcn_perm(v[i + 1], v[i], 0x05040100); };      // the left column's two rows
+  auto high = [&](int i) { return __builtin_amdgcn_perm(v[i + 1], v[i], 0x07060302); };
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     u32x4 a, b;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t* x = v + 16 * k + 4 * j;
-      const uint32_t l0 = __builtin_amdgcn_perm(x[1], x[0], 0x05040100), l1 = __builtin_amdgcn_perm(x[3], x[2], 0x05040100);
-      const uint32_t h0 = __builtin_amdgcn_perm(x[1], x[0], 0x07060302), h1 = __builtin_amdgcn_perm(x[3], x[2], 0x07060302);
-      a[j] = odd_values ? encode4_any(l0, l1, s0) : encode4(l0, l1, s0);
-      b[j] = odd_values ? encode4_any(h0, h1, s1) : encode4(h0, h1, s1);
+      a[j] = encode4(low(16 * k + 4 * j), low(16 * k + 4 * j + 2), s0);
+      b[j] = encode4(high(16 * k + 4 * j), high(16 * k + 4 * j + 2), s1);
+    }
+    if (odd_values) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        a[j] = mark_not_finite(a[j], low(16 * k + 4 * j), low(16 * k + 4 * j + 2));
+        b[j] = mark_not_finite(b[j], high(16 * k + 4 * j), high(16 * k + 4 * j + 2));
+      }
     }
     const int at = 16 * ((2 * quarter + k) ^ (pair & 7));
     *reinterpret_cast<u32x4*>(codes_t + (2 * pair) * FB + at) = a;
@@ -227,12 +241,8 @@ hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x
     if (q) hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_tile_kernel<true>), dim3(tiles), dim3(256), 0, s, g);
     else hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_tile_kernel<false>), dim3(tiles), dim3(256), 0, s, g);
   } else {
-    // four rows in flight per lane where that leaves enough waves
     const int64_t quads = g.S / 4;
-    if (R * quads >= 16384)
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_rows_kernel<4>), dim3((unsigned)((R + 15) / 16 * quads)), dim3(256), 0, s, g);
-    else
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(fp8_quantize_rows_kernel<1>), dim3((unsigned)((R + 3) / 4 * quads)), dim3(256), 0, s, g);
+    hipLaunchKernelGGL(fp8_quantize_rows_kernel, dim3((unsigned)((R + 4 * QR_ROWS - 1) / (4 * QR_ROWS) * quads)), dim3(256), 0, s, g);
   }
   return hipGetLastError();
 }

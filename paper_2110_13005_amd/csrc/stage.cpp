@@ -2146,8 +2146,8 @@ static constexpr int64_t kMaxRows = 1 << 24;
 
 static int embedding_sizes(const char* what, int64_t T, int64_t h, int64_t vocab) {
   if (T < 1 || h < 1 || vocab < 1) return fail(AXONN_EINVAL, "%s: non-positive size", what);
-  if (T > kMaxRows || h > 65535 || vocab > (1 << 30) || vocab * h > (int64_t(1) << 34))
-    return fail(AXONN_EUNSUPPORTED, "%s: at most 2^24 tokens, h 65535, vocab 2^30 and vocab * h 2^34", what);
+  if (T > kMaxRows || h > 65535 || vocab > kMaxRows || vocab * h > (int64_t(1) << 34))
+    return fail(AXONN_EUNSUPPORTED, "%s: at most 2^24 tokens, h 65535, vocab 2^24 and vocab * h 2^34", what);
   return AXONN_OK;
 }
 
@@ -2262,8 +2262,8 @@ int axonn_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x, void* 
   if ((q == nullptr) != (scale == nullptr) || (q_t == nullptr) != (scale_t == nullptr) || (!q && !q_t))
     return fail(AXONN_EINVAL, "fp8_quantize: codes and scales of one form at least, each with the other");
   if (R < 1 || C < 1) return fail(AXONN_EINVAL, "fp8_quantize: non-positive size");
-  if (R > (1 << 22) || C > (1 << 22) || R * C > (int64_t(1) << 36))
-    return fail(AXONN_EUNSUPPORTED, "fp8_quantize: dimension above 2^22 or more than 2^36 elements");
+  if (R > (1 << 22) || C > (1 << 22) || R * C > (int64_t(1) << 35))
+    return fail(AXONN_EUNSUPPORTED, "fp8_quantize: dimension above 2^22 or more than 2^35 elements");
   if (ld_x < C) return fail(AXONN_EINVAL, "fp8_quantize: ld_x < C");
   if ((uintptr_t)q % 16 || (uintptr_t)q_t % 16 || (uintptr_t)scale % 4 || (uintptr_t)scale_t % 4)
     return fail(AXONN_EINVAL, "fp8_quantize: codes must be 16-byte aligned, scales 4-byte aligned");

@@ -39,7 +39,7 @@ def test_embedding():
     refused(INV, B.axonn_embedding_bwd, *with_args(ok, _5=7))
     refused(INV, B.axonn_embedding_bwd, *with_args(ok, _10=A + 8))
     refused(INV, B.axonn_embedding_bwd, *with_args(ok, _7=A + 2, _8=1))
-    refused(UNS, B.axonn_embedding_bwd, *with_args(ok, _2=1 << 31))
+    refused(UNS, B.axonn_embedding_bwd, *with_args(ok, _2=(1 << 24) + 1))
     refused(INV, B.axonn_embedding_bwd_workspace, 0, 8, 10)
     assert B.load().axonn_embedding_bwd_workspace(4, 8, 10, None) == INV
     assert B.axonn_embedding_bwd_workspace(4, 8, 10) >= 16
