@@ -100,6 +100,7 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_scatter_kernel(co
     const int b = b0 + tid;
     uint32_t total = 0, before = 0;
     if (b < bins)
+#pragma unroll 8
       for (int q = 0; q < blocks; ++q) {
         const uint32_t v = p.hist[(int64_t)q * bins + b];
         total += v;
@@ -170,76 +171,130 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_scatter_kernel(co
   }
 }
 
-// Up to SORT_ONE_MAX tokens in one workgroup, in LDS, where id and token index together fit 32 bits; the other workgroups of the
-// launch clear the table meanwhile.  Each pass as in the scatter kernel above: a wave owns 64 * SORT_ONE_ITEMS consecutive places.
-constexpr int SORT_ONE_THREADS = 1024, SORT_ONE_WAVES = SORT_ONE_THREADS / 64, SORT_ONE_ITEMS = 16;
-constexpr int SORT_ONE_MAX = SORT_ONE_THREADS * SORT_ONE_ITEMS, SORT_ONE_BITS = 9;
+// Up to SORT_RANGE_MAX tokens in one launch: a workgroup per range of ids looks at all tokens, counts those below its range (its
+// place in the list) and sorts those in it, in LDS: id and token index as one 32-bit key, one pass per digit as in the scatter
+// kernel, none if they are all the same.  The launch's other workgroups clear the table meanwhile.  A workgroup that sorted
+// all ids by itself was bound by its ballots: 30 us for 16384 tokens.
+constexpr int SORT_RANGE_THREADS = 1024, SORT_RANGE_WAVES = SORT_RANGE_THREADS / 64, SORT_RANGE_ITEMS = 16;
+constexpr int SORT_RANGE_MAX = SORT_RANGE_THREADS * SORT_RANGE_ITEMS, SORT_RANGE_BITS = 8, SORT_RANGES = 32;
 
-// Zeros to `halves` 16-bit numbers from p on, by workgroup `block` of `blocks`.
+// Zeros to `halves` 16-bit numbers from p on, by workgroup `block` of `blocks`: four chunks per thread and round.
 template <int THREADS>
 __device__ __forceinline__ void clear_table(uint16_t* p, int64_t halves, int64_t block, int64_t blocks) {
-  for (int64_t i = (block * THREADS + threadIdx.x) * 8; i < halves; i += blocks * (THREADS * 8))
-    store_chunk((elem_t*)(p + i), elemx8{}, (int)min((int64_t)8, halves - i));
+  constexpr int64_t ROUND = THREADS * 8 * 4;
+  for (int64_t i0 = block * ROUND; i0 < halves; i0 += blocks * ROUND) {
+    const int64_t i = i0 + threadIdx.x * 8;
+    if (i0 + ROUND <= halves) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *reinterpret_cast<elemx8_any*>(p + i + k * (THREADS * 8)) = elemx8{};
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < 4; ++k) {
+        const int64_t at = i + k * (THREADS * 8);
+        if (at < halves) store_chunk((elem_t*)(p + at), elemx8{}, (int)min((int64_t)8, halves - at));
+      }
+    }
+  }
 }
 
-__global__ __launch_bounds__(SORT_ONE_THREADS) void embedding_sort_one_kernel(int T, int vocab, int bits, int t_bits, const int* __restrict__ tokens,
-                                                                              int* __restrict__ ids, int* __restrict__ order, uint16_t* clear,
-                                                                              int64_t halves) {
-  constexpr int BINS = 1 << SORT_ONE_BITS;
-  __shared__ uint32_t list[SORT_ONE_MAX];
-  __shared__ uint32_t counter[SORT_ONE_WAVES][BINS];
-  __shared__ uint32_t wave_total[BINS / 64];
-  if (blockIdx.x > 0) {
-    clear_table<SORT_ONE_THREADS>(clear, halves, blockIdx.x - 1, gridDim.x - 1);
+__global__ __launch_bounds__(SORT_RANGE_THREADS) void embedding_sort_range_kernel(int T, int vocab, int range_bits, int ranges, int t_bits,
+                                                                                  const int* __restrict__ tokens, int* __restrict__ ids,
+                                                                                  int* __restrict__ order, uint16_t* clear, int64_t halves) {
+  constexpr int BINS = 1 << SORT_RANGE_BITS;
+  __shared__ uint32_t list[SORT_RANGE_MAX];
+  __shared__ uint32_t counter[SORT_RANGE_WAVES][BINS];
+  __shared__ uint32_t wave_sum[SORT_RANGE_WAVES], wave_below[SORT_RANGE_WAVES];
+  if ((int)blockIdx.x >= ranges) {
+    clear_table<SORT_RANGE_THREADS>(clear, halves, blockIdx.x - ranges, gridDim.x - ranges);
     return;
   }
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int items = (T + SORT_ONE_THREADS - 1) / SORT_ONE_THREADS, first = wave * 64 * items + lane;
-  uint32_t key[SORT_ONE_ITEMS], rank[SORT_ONE_ITEMS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t range = blockIdx.x;
+  // the tokens of this range, in order: wave w looks at 64 * looks consecutive ones
+  const int looks = (T + SORT_RANGE_THREADS - 1) / SORT_RANGE_THREADS;
+  int id[SORT_RANGE_ITEMS];
+  uint32_t taken = 0, below = 0;
 #pragma unroll
-  for (int k = 0; k < SORT_ONE_ITEMS; ++k) {
-    const int i = first + 64 * k;
-    key[k] = k < items && i < T ? (uint32_t)clamp_token(tokens[i], vocab) << t_bits | (uint32_t)i : 0;
+  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+    const int i = (wave * looks + k) * 64 + lane;
+    id[k] = k < looks && i < T ? clamp_token(tokens[i], vocab) : 0x7fffffff;
   }
-  for (int shift = 0; shift < bits; shift += SORT_ONE_BITS) {
-    const int digit_bits = min(SORT_ONE_BITS, bits - shift), at = t_bits + shift;
-    for (int b = tid; b < SORT_ONE_WAVES * BINS; b += SORT_ONE_THREADS) (&counter[0][0])[b] = 0;
+#pragma unroll
+  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+    taken += __popcll(__ballot((uint32_t)id[k] >> range_bits == range));
+    below += __popcll(__ballot((uint32_t)id[k] >> range_bits < range));
+  }
+  if (lane == 0) {
+    wave_sum[wave] = taken;
+    wave_below[wave] = below;
+  }
+  __syncthreads();
+  uint32_t at = 0, n = 0, base = 0;
+  for (int w = 0; w < SORT_RANGE_WAVES; ++w) {
+    if (w < wave) at += wave_sum[w];
+    n += wave_sum[w];
+    base += wave_below[w];
+  }
+  if (n == 0) return;
+#pragma unroll
+  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+    const bool in = (uint32_t)id[k] >> range_bits == range;
+    const unsigned long long m = __ballot(in);
+    if (in) list[at + __popcll(m & ((1ull << lane) - 1))] = (uint32_t)id[k] << t_bits | (uint32_t)((wave * looks + k) * 64 + lane);
+    at += __popcll(m);
+  }
+  __syncthreads();
+  // sort list[0 .. n): wave w owns 64 * items consecutive places
+  const int items = ((int)n + SORT_RANGE_THREADS - 1) / SORT_RANGE_THREADS, first = wave * 64 * items + lane;
+  uint32_t key[SORT_RANGE_ITEMS], rank[SORT_RANGE_ITEMS];
+  bool other = false;
+  const uint32_t some = list[0] >> t_bits;
+#pragma unroll
+  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+    const int i = first + 64 * k;
+    key[k] = k < items && i < (int)n ? list[i] : 0;
+    other |= k < items && i < (int)n && key[k] >> t_bits != some;
+  }
+  const bool unsorted = __syncthreads_or(other);
+  for (int shift = 0; unsorted && shift < range_bits; shift += SORT_RANGE_BITS) {
+    const int digit_bits = min(SORT_RANGE_BITS, range_bits - shift), low = t_bits + shift;
+    for (int b = tid; b < SORT_RANGE_WAVES * BINS; b += SORT_RANGE_THREADS) (&counter[0][0])[b] = 0;
     __syncthreads();
     volatile uint32_t* const mine = counter[wave];
 #pragma unroll
-    for (int k = 0; k < SORT_ONE_ITEMS; ++k) {
-      const bool live = first + 64 * k < T;            // k < items where any lane is
+    for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
       if (k >= items) continue;
-      const uint32_t digit = key[k] >> at & ((1u << digit_bits) - 1);
+      const bool live = first + 64 * k < (int)n;
+      const uint32_t digit = key[k] >> low & ((1u << digit_bits) - 1);
       unsigned long long peers = __ballot(live);
       for (int bit = 0; bit < digit_bits; ++bit) {
         const unsigned long long set = __ballot(digit >> bit & 1);
         peers &= digit >> bit & 1 ? set : ~set;
       }
-      const unsigned long long below = peers & ((1ull << lane) - 1);
+      const unsigned long long in_front = peers & ((1ull << lane) - 1);
       const uint32_t old = live ? mine[digit] : 0;
-      rank[k] = old + __popcll(below);
+      rank[k] = old + __popcll(in_front);
       __builtin_amdgcn_wave_barrier();                 // every lane has read before the first of a digit's lanes writes
-      if (live && below == 0) mine[digit] = old + __popcll(peers);
+      if (live && in_front == 0) mine[digit] = old + __popcll(peers);
       __builtin_amdgcn_wave_barrier();
     }
     __syncthreads();
     // counters -> places: exclusive over the digits, then over the waves
     uint32_t total = 0, scan = 0;
-    if (tid < BINS) {
-      for (int w = 0; w < SORT_ONE_WAVES; ++w) total += counter[w][tid];
+    if (wave < BINS / 64) {
+      for (int w = 0; w < SORT_RANGE_WAVES; ++w) total += counter[w][tid];
       scan = total;
       for (int o = 1; o < 64; o <<= 1) {
         const uint32_t up = __shfl_up(scan, o, 64);
         if (lane >= o) scan += up;
       }
-      if (lane == 63) wave_total[wave] = scan;
+      if (lane == 63) wave_sum[wave] = scan;
     }
     __syncthreads();
-    if (tid < BINS) {
+    if (wave < BINS / 64) {
       uint32_t place = scan - total;
-      for (int w = 0; w < wave; ++w) place += wave_total[w];
-      for (int w = 0; w < SORT_ONE_WAVES; ++w) {
+      for (int w = 0; w < wave; ++w) place += wave_sum[w];
+      for (int w = 0; w < SORT_RANGE_WAVES; ++w) {
         const uint32_t c = counter[w][tid];
         counter[w][tid] = place;
         place += c;
@@ -247,27 +302,28 @@ __global__ __launch_bounds__(SORT_ONE_THREADS) void embedding_sort_one_kernel(in
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < SORT_ONE_ITEMS; ++k)
-      if (k < items && first + 64 * k < T) list[mine[key[k] >> at & ((1u << digit_bits) - 1)] + rank[k]] = key[k];
+    for (int k = 0; k < SORT_RANGE_ITEMS; ++k)
+      if (k < items && first + 64 * k < (int)n) list[mine[key[k] >> low & ((1u << digit_bits) - 1)] + rank[k]] = key[k];
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < SORT_ONE_ITEMS; ++k)
-      if (k < items && first + 64 * k < T) key[k] = list[first + 64 * k];
+    for (int k = 0; k < SORT_RANGE_ITEMS; ++k)
+      if (k < items && first + 64 * k < (int)n) key[k] = list[first + 64 * k];
   }
 #pragma unroll
-  for (int k = 0; k < SORT_ONE_ITEMS; ++k)
-    if (k < items && first + 64 * k < T) {
-      ids[first + 64 * k] = (int)(key[k] >> t_bits);
-      order[first + 64 * k] = (int)(key[k] & ((1u << t_bits) - 1));
+  for (int k = 0; k < SORT_RANGE_ITEMS; ++k)
+    if (k < items && first + 64 * k < (int)n) {
+      ids[base + first + 64 * k] = (int)(key[k] >> t_bits);
+      order[base + first + 64 * k] = (int)(key[k] & ((1u << t_bits) - 1));
     }
 }
 
 // --------------------------------------------------------------------------------------------------------------- sums
-// The sorted list is cut into pieces of PIECE tokens; a wave adds the rows of one piece over 512 columns (8 per lane), all
-// of them in flight.  A run of equal ids that lies within the piece is finished here; one that crosses the piece's start
+// The sorted list is cut into pieces; a wave adds the rows of one piece over 512 columns (8 per lane), SUM_BATCH of them in
+// flight.  Pieces are one batch, or four where there are many tokens: fewer sums of runs that cross pieces.  A run of equal ids that lies within the piece is finished here; one that crosses the piece's start
 // leaves its sum in partial[piece][0], one that begins in the piece and crosses its end in partial[piece][1], and
 // embedding_bwd_join_kernel adds them up.
-constexpr int PIECE = 16, SUM_COLS = 512;
+constexpr int SUM_BATCH = 16, SUM_COLS = 512;
+constexpr int PIECE_FEW = SUM_BATCH, PIECE_MANY = 4 * SUM_BATCH, MANY_TOKENS = 32768;
 typedef floatx4 floatx4_any __attribute__((aligned(4)));
 
 struct TableGrad {
@@ -315,7 +371,7 @@ __device__ __forceinline__ void add_chunk(float (&acc)[8], const elemx8& v) {
   for (int e = 0; e < 8; ++e) acc[e] += (float)v[e];
 }
 
-template <bool FP32>
+template <bool FP32, int PIECE>
 __global__ __launch_bounds__(256) void embedding_bwd_sum_kernel(const TableGrad g) {
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -325,52 +381,56 @@ __global__ __launch_bounds__(256) void embedding_bwd_sum_kernel(const TableGrad 
   const int mine = first + min(lane, count - 1);
   const int lane_id = g.ids[mine], lane_row = g.order[mine];
   const int before = first > 0 ? g.ids[first - 1] : -1, behind = first + count < g.T ? g.ids[first + count] : -1;
-  // Ids and rows as scalars, in front of every branch that lanes take differently: in such a branch the registers of lanes that
-  // are not in it may hold anything.  Places past the last token repeat it, and are not added.
-  int id[PIECE + 1], row[PIECE];
-#pragma unroll
-  for (int k = 0; k < PIECE; ++k) {
-    id[k] = __builtin_amdgcn_readlane(lane_id, k);
-    row[k] = __builtin_amdgcn_readlane(lane_row, k);
-  }
-  id[PIECE] = behind;
-  elemx8 v[PIECE];
-  if (n >= 8) {
-#pragma unroll
-    for (int k = 0; k < PIECE; ++k) v[k] = *reinterpret_cast<const elemx8_any*>(g.dout + (int64_t)row[k] * g.ld_dout + c);
-  } else if (n > 0) {
-    // the lane of the last, shorter chunk, element by element
-#pragma unroll
-    for (int k = 0; k < PIECE; ++k) v[k] = load_chunk(g.dout + (int64_t)row[k] * g.ld_dout + c, n);
-  }
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
   bool from_start = true;                               // the run at hand began with the piece
+#pragma unroll 1
+  for (int b = 0; b < count; b += SUM_BATCH) {
+    // Ids and rows as scalars, in front of every branch that lanes take differently: in such a branch the registers of lanes that
+    // are not in it may hold anything.  Places past the last token repeat it, and are not added.
+    int id[SUM_BATCH + 1], row[SUM_BATCH];
 #pragma unroll
-  for (int i = 0; i < PIECE; ++i) {
-    if (i < count) {
-      const int cur = id[i], next = i + 1 < count ? id[i + 1] : behind;
-      add_chunk(acc, v[i]);
-      if (next != cur || i + 1 == count) {
-        const bool head = from_start && before == cur, tail = next == cur;
-        if (n > 0) {
-          if (!head && !tail) store_table_row<FP32>(g, cur, c, n, acc);
-          else {
-            float* p = g.partial + ((int64_t)piece * 2 + (head ? 0 : 1)) * g.h + c;
-            if (n >= 8) {
-              ((floatx4_any*)p)[0] = floatx4{acc[0], acc[1], acc[2], acc[3]};
-              ((floatx4_any*)p)[1] = floatx4{acc[4], acc[5], acc[6], acc[7]};
-            } else {
+    for (int k = 0; k < SUM_BATCH; ++k) {
+      id[k] = __builtin_amdgcn_readlane(lane_id, b + k);
+      row[k] = __builtin_amdgcn_readlane(lane_row, b + k);
+    }
+    id[SUM_BATCH] = b + SUM_BATCH < count ? __builtin_amdgcn_readlane(lane_id, min(b + SUM_BATCH, 63)) : behind;
+    elemx8 v[SUM_BATCH];
+    if (n >= 8) {
 #pragma unroll
-              for (int e = 0; e < 7; ++e)
-                if (e < n) p[e] = acc[e];
+      for (int k = 0; k < SUM_BATCH; ++k) v[k] = *reinterpret_cast<const elemx8_any*>(g.dout + (int64_t)row[k] * g.ld_dout + c);
+    } else if (n > 0) {
+      // the lane of the last, shorter chunk, element by element
+#pragma unroll
+      for (int k = 0; k < SUM_BATCH; ++k) v[k] = load_chunk(g.dout + (int64_t)row[k] * g.ld_dout + c, n);
+    }
+#pragma unroll
+    for (int i = 0; i < SUM_BATCH; ++i) {
+      if (b + i < count) {
+        const bool final = b + i + 1 == count;
+        const int cur = id[i], next = final ? behind : id[i + 1];
+        add_chunk(acc, v[i]);
+        if (next != cur || final) {
+          const bool head = from_start && before == cur, tail = next == cur;
+          if (n > 0) {
+            if (!head && !tail) store_table_row<FP32>(g, cur, c, n, acc);
+            else {
+              float* p = g.partial + ((int64_t)piece * 2 + (head ? 0 : 1)) * g.h + c;
+              if (n >= 8) {
+                ((floatx4_any*)p)[0] = floatx4{acc[0], acc[1], acc[2], acc[3]};
+                ((floatx4_any*)p)[1] = floatx4{acc[4], acc[5], acc[6], acc[7]};
+              } else {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                  if (e < n) p[e] = acc[e];
+              }
             }
           }
-        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-        from_start = false;
+          for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+          from_start = false;
+        }
       }
     }
   }
@@ -378,7 +438,7 @@ __global__ __launch_bounds__(256) void embedding_bwd_sum_kernel(const TableGrad 
 
 // Runs that cross pieces.  One workgroup per piece and 512 columns; it has work if a run begins in its piece and crosses the
 // end.  The run's parts in the following pieces are shared out to the four waves in order, and the waves' sums added in order.
-template <bool FP32>
+template <bool FP32, int PIECE>
 __global__ __launch_bounds__(256) void embedding_bwd_join_kernel(const TableGrad g) {
   __shared__ float sums[3][64][8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), piece = blockIdx.x;
@@ -441,21 +501,21 @@ __global__ __launch_bounds__(256) void embedding_bwd_join_kernel(const TableGrad
   store_table_row<FP32>(g, id, c, n, acc);
 }
 
-// Up to FEW_MAX tokens: no sort, one launch, every row of the result has one writer.  A workgroup takes ROWS rows of the table
-// (accumulating: the ids of ROWS tokens, those that no earlier token has) and 512 columns, marks in bit masks which tokens
-// name them, and its waves add the marked rows of dout in token order, eight in flight; the tokens of a row with many are
-// shared out to the four waves.  Rows without tokens are cleared.
-constexpr int FEW_MAX = 1024, FEW_SHARED = 32;
+// Up to FEW_MAX tokens: no sort, and every row of the result has one writer.  A workgroup takes ROWS rows and 512 columns, marks
+// in bit masks which tokens name them, and its waves add the marked rows of dout in token order, eight in flight; the tokens
+// of a row with many are shared out to the four waves.  The rows are those of the table in turn (`all`: rows without tokens are
+// cleared, so this is the only launch), or the ids of ROWS tokens that no earlier token has.
+constexpr int FEW_MAX = 256, FEW_SHARED = 32;
 template <bool FP32, int ROWS>
-__global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const TableGrad g) {
+__global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const TableGrad g, int all) {
   __shared__ unsigned long long mask[ROWS][FEW_MAX / 64];
   __shared__ float sums[3][64][8];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r0 = blockIdx.x * ROWS, c = blockIdx.y * SUM_COLS + 8 * lane, n = g.h - c, words = (g.T + 63) / 64;
   auto row_id = [&](int r) {                            // -1: none
     const int i = r0 + r;
-    if (g.accumulate) return i < g.T ? clamp_token(g.ids[i], g.vocab) : -1;
-    return i < g.vocab ? i : -1;
+    if (all) return i < g.vocab ? i : -1;
+    return i < g.T ? clamp_token(g.ids[i], g.vocab) : -1;
   };
   int want[ROWS];
 #pragma unroll
@@ -504,7 +564,7 @@ __global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const TableGrad 
     for (int w = 0; w < words; ++w) {
       const unsigned long long m = mask[r][w];
       tokens += __popcll(m);
-      if (g.accumulate && w * 64 < r0 + r) earlier |= (w * 64 + 64 <= r0 + r ? m : m & ((1ull << ((r0 + r) & 63)) - 1)) != 0;
+      if (!all && w * 64 < r0 + r) earlier |= (w * 64 + 64 <= r0 + r ? m : m & ((1ull << ((r0 + r) & 63)) - 1)) != 0;
     }
     if (earlier) continue;
     const bool shared = tokens > FEW_SHARED;            // the same for the whole workgroup
@@ -550,9 +610,10 @@ static EmbeddingWs embedding_ws(int64_t T, int64_t h, int64_t vocab) {
   if (T > FEW_MAX) {
     const int64_t tiles = (T + SORT_TILE - 1) / SORT_TILE;
     const int64_t per = (tiles + SORT_MAX_BLOCKS - 1) / SORT_MAX_BLOCKS;
+    const int piece = T >= MANY_TOKENS ? PIECE_MANY : PIECE_FEW;
     w.per_block = (int)(per * SORT_TILE);
     w.blocks = (int)((tiles + per - 1) / per);
-    w.pieces = (int)((T + PIECE - 1) / PIECE);
+    w.pieces = (int)((T + piece - 1) / piece);
     for (int i = 0; i < 2; ++i) { w.keys[i] = take(4 * (uint64_t)T); w.index[i] = take(4 * (uint64_t)T); }
     w.hist = take(4ull * w.blocks << SORT_MAX_BITS);
     w.partial = take(8ull * w.pieces * (uint64_t)h);
@@ -562,31 +623,41 @@ static EmbeddingWs embedding_ws(int64_t T, int64_t h, int64_t vocab) {
 }
 uint64_t embedding_bwd_ws_bytes(int64_t T, int64_t h, int64_t vocab) { return embedding_ws(T, h, vocab).bytes; }
 
+template <bool FP32, int PIECE>
+static void launch_embedding_sums(const TableGrad& g, hipStream_t s) {
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_sum_kernel<FP32, PIECE>), dim3((unsigned)(((int64_t)g.pieces * g.col_chunks + 3) / 4)),
+                     dim3(256), 0, s, g);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_join_kernel<FP32, PIECE>), dim3(g.pieces, g.col_chunks), dim3(256), 0, s, g);
+}
+
 template <bool FP32>
 static hipError_t launch_embedding_bwd_t(TableGrad g, const EmbeddingWs& w, const int* tokens, char* ws, hipStream_t s) {
   const int64_t T = g.T, halves = (int64_t)g.vocab * g.h * (FP32 ? 2 : 1);
+  auto clear = [&]() {
+    hipLaunchKernelGGL(embedding_clear_kernel, dim3((unsigned)std::min<int64_t>(1 << 20, (halves + 8191) / 8192)), dim3(256), 0, s,
+                       (uint16_t*)g.dtable, halves);
+  };
   if (T <= FEW_MAX) {
     g.ids = tokens;
-    const int64_t rows = g.accumulate ? T : g.vocab;
-    // more rows per workgroup where there are workgroups enough: each looks at every token once
-    if (rows > 8192)
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_few_kernel<FP32, 16>), dim3((unsigned)((rows + 15) / 16), g.col_chunks), dim3(256), 0, s, g);
-    else
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_few_kernel<FP32, 4>), dim3((unsigned)((rows + 3) / 4), g.col_chunks), dim3(256), 0, s, g);
+    // rows of a small table one by one (every workgroup looks at every token), else the table cleared by a launch of its own
+    const bool all = !g.accumulate && g.vocab <= 2048;
+    if (!g.accumulate && !all) clear();
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_few_kernel<FP32, 4>), dim3((unsigned)(((all ? g.vocab : T) + 3) / 4), g.col_chunks), dim3(256),
+                       0, s, g, (int)all);
     return hipGetLastError();
   }
   int t_bits = 1;
   while (((int64_t)1 << t_bits) < T) ++t_bits;
-  if (T <= SORT_ONE_MAX && w.bits + t_bits <= 32) {
-    // a workgroup of the clearing part has 16 KB at least
-    const int64_t clearing = g.accumulate ? 0 : std::min<int64_t>(1024, (halves + 8191) / 8192);
-    hipLaunchKernelGGL(embedding_sort_one_kernel, dim3((unsigned)(1 + clearing)), dim3(SORT_ONE_THREADS), 0, s, g.T, g.vocab, w.bits, t_bits, tokens,
-                       (int*)(ws + w.keys[0]), (int*)(ws + w.index[0]), (uint16_t*)g.dtable, halves);
+  if (T <= SORT_RANGE_MAX && w.bits + t_bits <= 32) {
+    int range_bits = 0;                                 // the fewest with which SORT_RANGES ranges cover the ids
+    while ((int64_t)SORT_RANGES << range_bits < g.vocab) ++range_bits;
+    const int ranges = (int)((((int64_t)g.vocab - 1) >> range_bits) + 1);
+    const int64_t clearing = g.accumulate ? 0 : std::min<int64_t>(1 << 20, (halves + 32767) / 32768);
+    hipLaunchKernelGGL(embedding_sort_range_kernel, dim3((unsigned)(ranges + clearing)), dim3(SORT_RANGE_THREADS), 0, s, g.T, g.vocab, range_bits,
+                       ranges, t_bits, tokens, (int*)(ws + w.keys[0]), (int*)(ws + w.index[0]), (uint16_t*)g.dtable, halves);
     g.ids = (const int*)(ws + w.keys[0]); g.order = (const int*)(ws + w.index[0]);
   } else {
-    if (!g.accumulate)
-      hipLaunchKernelGGL(embedding_clear_kernel, dim3((unsigned)std::min<int64_t>(4096, (halves + 2047) / 2048)), dim3(256), 0, s,
-                         (uint16_t*)g.dtable, halves);
+    if (!g.accumulate) clear();
     const int passes = (w.bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS;
     for (int i = 0, shift = 0; i < passes; ++i) {
       SortPass p;
@@ -607,9 +678,8 @@ static hipError_t launch_embedding_bwd_t(TableGrad g, const EmbeddingWs& w, cons
     g.ids = (const int*)(ws + w.keys[(passes - 1) & 1]); g.order = (const int*)(ws + w.index[(passes - 1) & 1]);
   }
   g.partial = (float*)(ws + w.partial);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_sum_kernel<FP32>), dim3((unsigned)(((int64_t)g.pieces * g.col_chunks + 3) / 4)), dim3(256), 0,
-                     s, g);
-  hipLaunchKernelGGL(HIP_KERNEL_NAME(embedding_bwd_join_kernel<FP32>), dim3(g.pieces, g.col_chunks), dim3(256), 0, s, g);
+  if (T >= MANY_TOKENS) launch_embedding_sums<FP32, PIECE_MANY>(g, s);
+  else launch_embedding_sums<FP32, PIECE_FEW>(g, s);
   return hipGetLastError();
 }
 
