@@ -10,17 +10,20 @@
 //
 // A head belongs to LPH lanes; a lane holds 8 pairs, a[8] and b[8]: of the rotated part, a chunk of the first half and the
 // chunk of the second half that it is paired with, or (interleaved) 16 consecutive elements; of the part that is not
-// rotated, 16 consecutive elements.  So every pair lies in one lane and all memory operations are chunks of 8 elements.
+// rotated, 16 consecutive elements.  So every pair lies in one lane and memory operations are chunks of 8 elements.
 #include "rows.h"
+#include "host_logic.h"
 #include <algorithm>
 
 namespace axonn {
 
-constexpr int QK_THREADS = 256;
+constexpr int QK_THREADS = 256, QK_BACKWARD_BLOCKS = 768;
 
 struct QkArgs {
   int T, seq, heads, kv, d, rot;
-  int items;                       // heads a token has work for: heads + kv, and the kv heads of V if they are copied
+  int blocks_q;                    // workgroups of the query heads; the others take the key heads (and V)
+  int copy_v;                      // not in place
+  uint32_t recip_q, recip_k;       // reciprocals of heads and 2 * kv
   int tokens;                      // of a workgroup's turn
   const elem_t *x, *dy;            // packed rows; upstream gradient (backward)
   elem_t* out;
@@ -29,41 +32,54 @@ struct QkArgs {
   float eps;
   const int* positions;
   const double* inv_freq;
-  float* partial;                  // backward: [workgroups][2][d]
+  float* partial;                  // backward: [workgroups][d]
 };
 
-// What a lane holds of a head.
-struct QkLane { int off_a, off_b, n_a, n_b, pair; };       // pair: first rotated pair, or -1
-template <bool INTERLEAVED>
+// How the chunks of a head's parts (rotated halves or pairs, and what is not rotated) come out: all whole; the last one of a part
+// shorter, and read as the part's last 8 elements (the ones that the chunk in front has as well are computed twice, to the same
+// values, and counted once); or a part has fewer than 8 elements, which are read one by one.
+enum QkChunks { QK_WHOLE, QK_OVERLAP, QK_SHORT };
+
+// What a lane holds of a head: chunks at off_a and off_b of n_a and n_b elements (QK_SHORT: up to 8, else 8 or none), the first
+// dup of which belong to another lane; first angles of their pairs, or -1.
+struct QkLane { int off_a, off_b, n_a, n_b, dup_a, dup_b, pair_a, pair_b; };
+template <bool INTERLEAVED, int CHUNKS>
 __device__ __forceinline__ QkLane qk_lane(int v, int d, int rot) {
   const int turned = (rot / 2 + 7) / 8;                     // lanes of the rotated part
+  const bool rotates = v < turned;
   QkLane l;
-  if (v < turned) {
-    l.pair = 8 * v;
-    l.off_a = INTERLEAVED ? 16 * v : 8 * v;
-    l.off_b = INTERLEAVED ? 16 * v + 8 : rot / 2 + 8 * v;
-    l.n_a = (INTERLEAVED ? rot : rot / 2) - l.off_a;
-    l.n_b = rot - l.off_b;
+  int end_a, end_b;
+  if (rotates && !INTERLEAVED) {
+    l.off_a = 8 * v;
+    l.off_b = rot / 2 + 8 * v;
+    end_a = rot / 2;
+    end_b = rot;
   } else {
-    l.pair = -1;
-    l.off_a = rot + 16 * (v - turned);
+    l.off_a = rotates ? 16 * v : rot + 16 * (v - turned);
     l.off_b = l.off_a + 8;
-    l.n_a = d - l.off_a;
-    l.n_b = d - l.off_b;
+    end_a = end_b = rotates ? rot : d;
   }
-  l.n_a = max(0, min(8, l.n_a));
-  l.n_b = max(0, min(8, l.n_b));
+  l.n_a = max(0, min(8, end_a - l.off_a));
+  l.n_b = max(0, min(8, end_b - l.off_b));
+  l.dup_a = l.dup_b = 0;
+  if (CHUNKS == QK_OVERLAP) {
+    if (l.n_a) { l.dup_a = 8 - l.n_a; l.off_a -= l.dup_a; l.n_a = 8; }
+    if (l.n_b) { l.dup_b = 8 - l.n_b; l.off_b -= l.dup_b; l.n_b = 8; }
+  }
+  l.pair_a = rotates ? (INTERLEAVED ? l.off_a / 2 : l.off_a) : -1;
+  l.pair_b = INTERLEAVED && l.n_b ? l.off_b / 2 : l.pair_a;
   return l;
 }
 
-// (a, b) of the lane turned by its angles (c, s); INVERSE: back.
+// (a, b) of the lane turned by its angles; INVERSE: back.
 template <bool INTERLEAVED, bool INVERSE>
-__device__ __forceinline__ void qk_turn(float (&a)[8], float (&b)[8], const float2* cs) {
+__device__ __forceinline__ void qk_turn(float (&a)[8], float (&b)[8], const float2* cs, const QkLane& l) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float& p = INTERLEAVED ? (i < 4 ? a[2 * i] : b[2 * i - 8]) : a[i];
     float& q = INTERLEAVED ? (i < 4 ? a[2 * i + 1] : b[2 * i - 7]) : b[i];
-    const float c = cs[i].x, s = INVERSE ? -cs[i].y : cs[i].y;
+    const float2 t = cs[INTERLEAVED && i >= 4 ? l.pair_b + i - 4 : l.pair_a + i];
+    const float c = t.x, s = INVERSE ? -t.y : t.y;
     const float np = p * c - q * s, nq = p * s + q * c;
     p = np;
     q = nq;
@@ -90,155 +106,209 @@ __device__ __forceinline__ void qk_angles(const QkArgs& g, int t0, int count, in
   }
 }
 
-template <int LPH, bool INTERLEAVED, bool BACKWARD>
-__global__ __launch_bounds__(QK_THREADS) void qk_norm_rope_kernel(const QkArgs g) {
+template <int CHUNKS>
+__device__ __forceinline__ elemx8 qk_load(const elem_t* p, int n) {
+  if (CHUNKS == QK_SHORT) return load_chunk(p, n);
+  return n ? *reinterpret_cast<const elemx8_any*>(p) : elemx8{};
+}
+template <int CHUNKS>
+__device__ __forceinline__ void qk_store(elem_t* p, const elemx8& v, int n) {
+  if (CHUNKS == QK_SHORT) store_chunk(p, v, n);
+  else if (n) *reinterpret_cast<elemx8_any*>(p) = v;
+}
+
+// A workgroup takes the query heads or the key heads (one gain, and backward one set of sums, in registers), the rows of
+// the next head are on their way while one is worked on.
+template <int LPH, bool INTERLEAVED, int CHUNKS, bool BACKWARD>
+__global__ __launch_bounds__(QK_THREADS, BACKWARD ? 3 : 5) void qk_norm_rope_kernel(const QkArgs g) {
   extern __shared__ float2 qk_cs[];
   constexpr int GROUPS = QK_THREADS / LPH;
   const int group = threadIdx.x / LPH, v = threadIdx.x % LPH;
-  const QkLane l = qk_lane<INTERLEAVED>(v, g.d, g.rot);
+  const bool is_q = (int)blockIdx.x < g.blocks_q;
+  const int block = is_q ? blockIdx.x : blockIdx.x - g.blocks_q, blocks = is_q ? g.blocks_q : gridDim.x - g.blocks_q;
+  const int items = is_q ? g.heads : 2 * g.kv, normed = is_q ? g.heads : g.kv;
+  const uint32_t recip = is_q ? g.recip_q : g.recip_k;
+  const int64_t col0 = is_q ? 0 : (int64_t)g.heads * g.d;
+  const QkLane l = qk_lane<INTERLEAVED, CHUNKS>(v, g.d, g.rot);
+  auto mine_a = [&](int e) { return CHUNKS != QK_OVERLAP || e >= l.dup_a; };
+  auto mine_b = [&](int e) { return CHUNKS != QK_OVERLAP || e >= l.dup_b; };
   const int pairs = (g.rot / 2 + 7) / 8 * 8;
   const float inv_d = 1.0f / (float)g.d;
-  float gq[2][8], gk[2][8], sum_q[2][8], sum_k[2][8];
+  float gain[2][8], sum[2][8];
   {
-    const elemx8 qa = load_chunk(g.gamma_q + l.off_a, l.n_a), qb = load_chunk(g.gamma_q + l.off_b, l.n_b);
-    const elemx8 ka = load_chunk(g.gamma_k + l.off_a, l.n_a), kb = load_chunk(g.gamma_k + l.off_b, l.n_b);
+    const elem_t* const gamma = is_q ? g.gamma_q : g.gamma_k;
+    const elemx8 a = qk_load<CHUNKS>(gamma + l.off_a, l.n_a), b = qk_load<CHUNKS>(gamma + l.off_b, l.n_b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      gq[0][e] = (float)qa[e]; gq[1][e] = (float)qb[e];
-      gk[0][e] = (float)ka[e]; gk[1][e] = (float)kb[e];
-      sum_q[0][e] = sum_q[1][e] = sum_k[0][e] = sum_k[1][e] = 0.f;
+      gain[0][e] = (float)a[e];
+      gain[1][e] = (float)b[e];
+      sum[0][e] = sum[1][e] = 0.f;
     }
   }
-  for (int t0 = blockIdx.x * g.tokens; t0 < g.T; t0 += gridDim.x * g.tokens) {
-    const int count = min(g.tokens, g.T - t0);
+  struct Item { elemx8 va, vb, xa, xb; int k, head; };
+  for (int t0 = block * g.tokens; t0 < g.T; t0 += blocks * g.tokens) {
+    const int count = min(g.tokens, g.T - t0), n = count * items;
+    auto load = [&](Item& w, int it) {
+      w.k = (int)host::recip_div((uint32_t)it, (uint32_t)items, recip);
+      w.head = it - w.k * items;
+      const int64_t t = t0 + w.k, at = col0 + (int64_t)w.head * g.d;
+      if (w.head >= normed && !g.copy_v) return;
+      const elem_t* const src = (BACKWARD ? g.dy + t * g.ld_dy : g.x + t * g.ld_x) + at;
+      w.va = qk_load<CHUNKS>(src + l.off_a, l.n_a);
+      w.vb = qk_load<CHUNKS>(src + l.off_b, l.n_b);
+      if (BACKWARD && w.head < normed) {
+        const elem_t* const xs = g.x + t * g.ld_x + at;
+        w.xa = qk_load<CHUNKS>(xs + l.off_a, l.n_a);
+        w.xb = qk_load<CHUNKS>(xs + l.off_b, l.n_b);
+      }
+    };
+    Item next;
+    if (group < n) load(next, group);
     __syncthreads();
     qk_angles(g, t0, count, pairs, qk_cs);
     __syncthreads();
-    for (int it = blockIdx.y * GROUPS + group; it < count * g.items; it += gridDim.y * GROUPS) {
-      const int k = it / g.items, head = it - k * g.items;
-      const int64_t t = t0 + k;
-      const elem_t* src = (BACKWARD ? g.dy + t * g.ld_dy : g.x + t * g.ld_x) + (int64_t)head * g.d;
-      elem_t* dst = g.out + t * g.ld_out + (int64_t)head * g.d;
-      const elemx8 va = load_chunk(src + l.off_a, l.n_a), vb = load_chunk(src + l.off_b, l.n_b);
-      if (head >= g.heads + g.kv) {                     // V
-        store_chunk(dst + l.off_a, va, l.n_a);
-        store_chunk(dst + l.off_b, vb, l.n_b);
+    for (int it = group; it < n; it += GROUPS) {
+      const Item w = next;
+      if (it + GROUPS < n) load(next, it + GROUPS);
+      elem_t* const dst = g.out + (int64_t)(t0 + w.k) * g.ld_out + col0 + (int64_t)w.head * g.d;
+      if (w.head >= normed) {                           // V; in place it is passed over, so that the sums keep their order
+        if (!g.copy_v) continue;
+        qk_store<CHUNKS>(dst + l.off_a, w.va, l.n_a);
+        qk_store<CHUNKS>(dst + l.off_b, w.vb, l.n_b);
         continue;
       }
-      const bool is_q = head < g.heads;
-      const float2* cs = qk_cs + k * pairs + l.pair;
+      const float2* const cs = qk_cs + w.k * pairs;
       float a[8], b[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) { a[e] = (float)va[e]; b[e] = (float)vb[e]; }
+      for (int e = 0; e < 8; ++e) { a[e] = (float)w.va[e]; b[e] = (float)w.vb[e]; }
       if constexpr (!BACKWARD) {
         float sq = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sq += a[e] * a[e] + b[e] * b[e];
+        for (int e = 0; e < 8; ++e) {
+          sq += mine_a(e) ? a[e] * a[e] : 0.f;
+          sq += mine_b(e) ? b[e] * b[e] : 0.f;
+        }
         const float r = rsqrtf(head_sum<LPH>(sq) * inv_d + g.eps);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          a[e] *= r * (is_q ? gq[0][e] : gk[0][e]);
-          b[e] *= r * (is_q ? gq[1][e] : gk[1][e]);
+          a[e] *= r * gain[0][e];
+          b[e] *= r * gain[1][e];
         }
-        if (l.pair >= 0) qk_turn<INTERLEAVED, false>(a, b, cs);
+        if (l.pair_a >= 0) qk_turn<INTERLEAVED, false>(a, b, cs, l);
       } else {
-        const elem_t* xs = g.x + t * g.ld_x + (int64_t)head * g.d;
-        const elemx8 xva = load_chunk(xs + l.off_a, l.n_a), xvb = load_chunk(xs + l.off_b, l.n_b);
-        if (l.pair >= 0) qk_turn<INTERLEAVED, true>(a, b, cs);
-        float sq = 0.f, dot = 0.f, xa[8], xb[8];
+        if (l.pair_a >= 0) qk_turn<INTERLEAVED, true>(a, b, cs, l);
+        float sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          xa[e] = (float)xva[e];
-          xb[e] = (float)xvb[e];
-          sq += xa[e] * xa[e] + xb[e] * xb[e];
-          dot += a[e] * (is_q ? gq[0][e] : gk[0][e]) * xa[e] + b[e] * (is_q ? gq[1][e] : gk[1][e]) * xb[e];
+          const float xa = mine_a(e) ? (float)w.xa[e] : 0.f, xb = mine_b(e) ? (float)w.xb[e] : 0.f;
+          sq += xa * xa + xb * xb;
+          dot += a[e] * gain[0][e] * xa + b[e] * gain[1][e] * xb;
         }
         const float r = rsqrtf(head_sum<LPH>(sq) * inv_d + g.eps);
         const float m = head_sum<LPH>(dot) * r * inv_d;                  // mean(w xh)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float ha = r * xa[e], hb = r * xb[e];
-          if (is_q) { sum_q[0][e] += a[e] * ha; sum_q[1][e] += b[e] * hb; }
-          else { sum_k[0][e] += a[e] * ha; sum_k[1][e] += b[e] * hb; }
-          a[e] = r * (a[e] * (is_q ? gq[0][e] : gk[0][e]) - ha * m);
-          b[e] = r * (b[e] * (is_q ? gq[1][e] : gk[1][e]) - hb * m);
+          const float ha = r * (float)w.xa[e], hb = r * (float)w.xb[e];
+          sum[0][e] += a[e] * ha;                       // (of elements that are another lane's as well: not looked at)
+          sum[1][e] += b[e] * hb;
+          a[e] = r * (a[e] * gain[0][e] - ha * m);
+          b[e] = r * (b[e] * gain[1][e] - hb * m);
         }
       }
       elemx8 oa, ob;
 #pragma unroll
       for (int e = 0; e < 8; ++e) { oa[e] = (elem_t)a[e]; ob[e] = (elem_t)b[e]; }
-      store_chunk(dst + l.off_a, oa, l.n_a);
-      store_chunk(dst + l.off_b, ob, l.n_b);
+      qk_store<CHUNKS>(dst + l.off_a, oa, l.n_a);
+      qk_store<CHUNKS>(dst + l.off_b, ob, l.n_b);
     }
   }
   if constexpr (BACKWARD) {
-    // the workgroup's sums of the gains' gradients: over its groups in order
+    // the workgroup's sums of the gain's gradient: over its groups in order
     __shared__ float part[GROUPS][LPH * 16];
-    float* const dst = g.partial + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * g.d;
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      __syncthreads();
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        part[group][v * 16 + e] = which ? sum_k[0][e] : sum_q[0][e];
-        part[group][v * 16 + 8 + e] = which ? sum_k[1][e] : sum_q[1][e];
-      }
-      __syncthreads();
-      for (int i = threadIdx.x; i < LPH * 16; i += QK_THREADS) {
-        const QkLane o = qk_lane<INTERLEAVED>(i / 16, g.d, g.rot);
-        const int e = i % 16, col = e < 8 ? o.off_a + e : o.off_b + e - 8;
-        if (e < 8 ? e >= o.n_a : e - 8 >= o.n_b) continue;
-        float sum = 0.f;
-        for (int q = 0; q < GROUPS; ++q) sum += part[q][i];
-        dst[which * g.d + col] = sum;
-      }
+    for (int e = 0; e < 8; ++e) {
+      part[group][v * 16 + e] = sum[0][e];
+      part[group][v * 16 + 8 + e] = sum[1][e];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < LPH * 16; i += QK_THREADS) {
+      const QkLane o = qk_lane<INTERLEAVED, CHUNKS>(i / 16, g.d, g.rot);
+      const int e = i & 7, col = (i & 8 ? o.off_b : o.off_a) + e;
+      if (e >= (i & 8 ? o.n_b : o.n_a) || e < (i & 8 ? o.dup_b : o.dup_a)) continue;
+      float total = 0.f;
+      for (int q = 0; q < GROUPS; ++q) total += part[q][i];
+      g.partial[(int64_t)blockIdx.x * g.d + col] = total;
     }
   }
 }
 
-// dgamma_q[c], dgamma_k[c]: the workgroups' sums in order; 16 rows of 16 columns at a time.
-__global__ __launch_bounds__(256) void qk_gain_sum_kernel(int blocks, int d, const float* __restrict__ partial, float* __restrict__ dgamma_q,
-                                                          float* __restrict__ dgamma_k) {
-  __shared__ float red[16][17];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), r0 = threadIdx.x >> 4;
+// dgamma_q (blockIdx.y = 0) and dgamma_k: the workgroups' sums in order, 16 columns and 64 rows of them at a time.
+__global__ __launch_bounds__(1024) void qk_gain_sum_kernel(int blocks_q, int blocks_k, int d, const float* __restrict__ partial,
+                                                           float* __restrict__ dgamma_q, float* __restrict__ dgamma_k) {
+  __shared__ float red[64][17];
+  const int c = threadIdx.x & 15, col = blockIdx.x * 16 + c, r0 = threadIdx.x >> 4;
+  const float* const p = partial + (blockIdx.y ? (int64_t)blocks_q * d : 0);
+  const int rows = blockIdx.y ? blocks_k : blocks_q;
   float sum = 0.f;
-  if (col < 2 * d)
-    for (int r = r0; r < blocks; r += 16) sum += partial[(int64_t)r * 2 * d + col];
-  red[r0][threadIdx.x & 15] = sum;
+  if (col < d) {
+#pragma unroll 8
+    for (int r = r0; r < rows; r += 64) sum += p[(int64_t)r * d + col];
+  }
+  red[r0][c] = sum;
   __syncthreads();
-  if (r0 == 0 && col < 2 * d) {
+  if (r0 == 0 && col < d) {
     float total = 0.f;
-    for (int q = 0; q < 16; ++q) total += red[q][threadIdx.x];
-    if (col < d) dgamma_q[col] = total;
-    else dgamma_k[col - d] = total;
+#pragma unroll
+    for (int q = 0; q < 64; ++q) total += red[q][c];
+    (blockIdx.y ? dgamma_k : dgamma_q)[col] = total;
   }
 }
 
-struct QkPlan { int lph, tokens, grid_x, grid_y; };
-static QkPlan qk_plan(int64_t T, int items, int d, int rot, bool backward) {
+struct QkPlan { int lph, tokens, blocks_q, blocks_k; };
+static QkPlan qk_plan(int64_t T, int heads, int kv, int d, int rot, bool backward) {
   QkPlan p;
   const int lanes = (rot / 2 + 7) / 8 + (d - rot + 15) / 16;
   p.lph = lanes <= 4 ? 4 : lanes <= 8 ? 8 : lanes <= 16 ? 16 : 32;
-  p.tokens = T >= 2048 ? 4 : 1;
-  p.grid_x = (int)std::min<int64_t>((T + p.tokens - 1) / p.tokens, backward ? 512 : 1 << 20);
-  p.grid_y = 1;
+  // tokens of a turn: four rounds of heads for every group of lanes, while there are 512 turns.  Measured, us, 1 / 2 / 4 / 8 tokens:
+  // 4096 x (32, 8 heads of 128) 28 / 22 / 20 / 20, 16384 x (16, 16 of 64) 75 / 49 / 41 / 39, 8192 x (40, 40 of 128)
+  // 103 / 104 / 105 / 110, 512 x (16, 4 of 128) 7.0 / 5.4 / 5.5 / 7.1.
+  p.tokens = 1;
+  while (p.tokens < 8 && p.tokens * std::min(heads, 2 * kv) < 4 * QK_THREADS / p.lph && T >= (p.tokens == 1 ? 64 : 1024 * p.tokens)) p.tokens *= 2;
+  const int64_t turns = (T + p.tokens - 1) / p.tokens;
+  int64_t q = turns, k = turns;
+  if (backward) {                                       // a row of sums per workgroup: shared out by the heads
+    q = std::min<int64_t>(turns, std::max<int64_t>(1, (int64_t)QK_BACKWARD_BLOCKS * heads / (heads + 2 * kv)));
+    k = std::min<int64_t>(turns, std::max<int64_t>(1, QK_BACKWARD_BLOCKS - q));
+  }
+  p.blocks_q = (int)q;
+  p.blocks_k = (int)k;
   return p;
 }
-// Rows of sums that the backward pass leaves, whatever the rotated part.
-uint64_t qk_norm_rope_bwd_ws_bytes(int64_t T, int d) { return 8ull * (uint64_t)d * (uint64_t)std::min<int64_t>(T, 512); }
+// Rows of sums that the backward pass leaves, whatever the heads and the rotated part.
+uint64_t qk_norm_rope_bwd_ws_bytes(int64_t T, int d) { return 4ull * (uint64_t)d * (uint64_t)std::min<int64_t>(2 * T, QK_BACKWARD_BLOCKS + 1); }
 
 template <bool BACKWARD>
-static hipError_t launch_qk(const QkArgs& g0, bool interleaved, hipStream_t s) {
-  QkArgs g = g0;
-  const QkPlan p = qk_plan(g.T, g.items, g.d, g.rot, BACKWARD);
+static hipError_t launch_qk(QkArgs g, bool interleaved, const QkPlan& p, hipStream_t s) {
   g.tokens = p.tokens;
+  g.blocks_q = p.blocks_q;
+  g.recip_q = host::recip_of((uint32_t)g.heads);
+  g.recip_k = host::recip_of(2u * (uint32_t)g.kv);
   const size_t lds = (size_t)p.tokens * ((g.rot / 2 + 7) / 8 * 8) * sizeof(float2);
+  const dim3 grid((unsigned)(p.blocks_q + p.blocks_k));
+  const int part = interleaved ? g.rot : g.rot / 2, rest = g.d - g.rot;
+  auto launch_as = [&](auto lph, auto pairwise, auto chunks) {
+    constexpr int LPH = decltype(lph)::value, CHUNKS = decltype(chunks)::value;
+    constexpr bool PAIRWISE = decltype(pairwise)::value;
+    hipLaunchKernelGGL(HIP_KERNEL_NAME(qk_norm_rope_kernel<LPH, PAIRWISE, CHUNKS, BACKWARD>), grid, dim3(QK_THREADS), lds, s, g);
+  };
+  auto launch_chunks = [&](auto lph, auto pairwise) {
+    if ((part > 0 && part < 8) || (rest > 0 && rest < 8)) launch_as(lph, pairwise, std::integral_constant<int, QK_SHORT>{});
+    else if (part % 8 || rest % 8) launch_as(lph, pairwise, std::integral_constant<int, QK_OVERLAP>{});
+    else launch_as(lph, pairwise, std::integral_constant<int, QK_WHOLE>{});
+  };
   auto launch = [&](auto lph) {
-    constexpr int LPH = decltype(lph)::value;
-    if (interleaved)
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(qk_norm_rope_kernel<LPH, true, BACKWARD>), dim3(p.grid_x, p.grid_y), dim3(QK_THREADS), lds, s, g);
-    else
-      hipLaunchKernelGGL(HIP_KERNEL_NAME(qk_norm_rope_kernel<LPH, false, BACKWARD>), dim3(p.grid_x, p.grid_y), dim3(QK_THREADS), lds, s, g);
+    if (interleaved) launch_chunks(lph, std::true_type{});
+    else launch_chunks(lph, std::false_type{});
   };
   if (p.lph == 4) launch(std::integral_constant<int, 4>{});
   else if (p.lph == 8) launch(std::integral_constant<int, 8>{});
@@ -251,11 +321,11 @@ hipError_t launch_qk_norm_rope_fwd(const QkShape& q, const void* qkv, int64_t ld
                                    const int* positions, const double* inv_freq, void* out, int64_t ld_out, hipStream_t s) {
   QkArgs g = {};
   g.T = (int)q.T; g.seq = q.seq; g.heads = q.heads; g.kv = q.kv; g.d = q.d; g.rot = q.rot;
-  g.items = q.heads + q.kv + (out == qkv ? 0 : q.kv);
+  g.copy_v = out != qkv;
   g.x = (const elem_t*)qkv; g.out = (elem_t*)out; g.ld_x = ld_qkv; g.ld_out = ld_out;
   g.gamma_q = (const elem_t*)gamma_q; g.gamma_k = (const elem_t*)gamma_k; g.eps = eps;
   g.positions = positions; g.inv_freq = inv_freq;
-  return launch_qk<false>(g, q.interleaved, s);
+  return launch_qk<false>(g, q.interleaved, qk_plan(q.T, q.heads, q.kv, q.d, q.rot, false), s);
 }
 
 hipError_t launch_qk_norm_rope_bwd(const QkShape& q, const void* dout, int64_t ld_dout, const void* qkv, int64_t ld_qkv, const void* gamma_q,
@@ -263,16 +333,16 @@ hipError_t launch_qk_norm_rope_bwd(const QkShape& q, const void* dout, int64_t l
                                    int64_t ld_dqkv, float* dgamma_q, float* dgamma_k, float* workspace, hipStream_t s) {
   QkArgs g = {};
   g.T = (int)q.T; g.seq = q.seq; g.heads = q.heads; g.kv = q.kv; g.d = q.d; g.rot = q.rot;
-  g.items = q.heads + q.kv + (dqkv == dout ? 0 : q.kv);
+  g.copy_v = dqkv != dout;
   g.x = (const elem_t*)qkv; g.dy = (const elem_t*)dout; g.out = (elem_t*)dqkv;
   g.ld_x = ld_qkv; g.ld_dy = ld_dout; g.ld_out = ld_dqkv;
   g.gamma_q = (const elem_t*)gamma_q; g.gamma_k = (const elem_t*)gamma_k; g.eps = eps;
   g.positions = positions; g.inv_freq = inv_freq;
   g.partial = workspace;
-  hipError_t e = launch_qk<true>(g, q.interleaved, s);
+  const QkPlan p = qk_plan(q.T, q.heads, q.kv, q.d, q.rot, true);
+  const hipError_t e = launch_qk<true>(g, q.interleaved, p, s);
   if (e != hipSuccess) return e;
-  const QkPlan p = qk_plan(q.T, g.items, q.d, q.rot, true);
-  hipLaunchKernelGGL(qk_gain_sum_kernel, dim3((2 * q.d + 15) / 16), dim3(256), 0, s, p.grid_x * p.grid_y, q.d, (const float*)workspace,
+  hipLaunchKernelGGL(qk_gain_sum_kernel, dim3((q.d + 15) / 16, 2), dim3(1024), 0, s, p.blocks_q, p.blocks_k, q.d, (const float*)workspace,
                      dgamma_q, dgamma_k);
   return hipGetLastError();
 }

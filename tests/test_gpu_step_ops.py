@@ -146,7 +146,8 @@ QK = [  # T, seq, heads, kv, d, rot, interleaved, positions, padding, shift
     (9, 4, 2, 2, 188, 188, 1, "none", 1, 1), (4, 4, 5, 5, 80, 48, 0, "far", 0, 0), (4, 2, 8, 1, 256, 256, 0, "none", 0, 0),
     (3, 3, 2, 1, 256, 254, 0, "far", 5, 0), (3, 3, 2, 1, 256, 2, 1, "far", 0, 0), (8, 8, 2, 1, 96, 0, 0, "none", 0, 0),
     (5, 5, 3, 3, 10, 6, 1, "signed", 1, 1), (2050, 1025, 2, 1, 64, 64, 0, "none", 0, 0), (2100, 2100, 1, 1, 20, 14, 0, "far", 0, 0),
-    (700, 700, 12, 4, 128, 128, 0, "none", 0, 0)]
+    (700, 700, 12, 4, 128, 128, 0, "none", 0, 0), (33, 33, 5, 2, 100, 60, 0, "far", 0, 0), (33, 11, 5, 2, 100, 60, 1, "none", 1, 0),
+    (20, 20, 3, 3, 36, 20, 1, "none", 0, 1), (20, 20, 3, 3, 46, 36, 0, "far", 0, 0), (70, 70, 40, 40, 128, 128, 0, "none", 0, 0)]
 
 
 @pytest.mark.parametrize("T,seq,heads,kv,d,rot,inter,positions,pad,shift", QK)
