@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(HERE, "libaxonn_stage.so")
 LIB_PATH_FP16 = os.path.join(HERE, "libaxonn_stage_fp16.so")
 VARIANTS = {"bf16": (LIB_PATH, []), "fp16": (LIB_PATH_FP16, ["-DAXONN_ELEM_FP16"])}
 SOURCES = ["gemm.hip", "attention.hip", "fp8.hip", "elementwise.hip", "lm_ends.hip", "stage.cpp", "qk_norm.hip", "embedding.hip",
-           "dropout.hip"]
+           "dropout.hip", "step_ops.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -8,10 +8,11 @@
 // which they are kept, so the rounding of p leaves the expectation as it is.
 #include "rows.h"
 #include "host_logic.h"
+#include <type_traits>
 
 namespace axonn {
 
-constexpr int DO_THREADS = 256, DO_CHUNKS = 4;       // chunks of 8 elements per lane
+constexpr int DO_THREADS = 256;
 
 struct DropoutArgs {
   int64_t n_chunks;                 // of all rows
@@ -37,7 +38,8 @@ __device__ __forceinline__ void philox4x32_10(uint32_t (&c)[4], uint32_t k0, uin
   }
 }
 
-template <bool RES>
+// DO_CHUNKS: chunks of 8 elements per lane.
+template <bool RES, int DO_CHUNKS>
 __global__ __launch_bounds__(DO_THREADS) void dropout_kernel(const DropoutArgs g) {
   const int64_t base = (int64_t)blockIdx.x * (DO_THREADS * DO_CHUNKS);
   const int64_t row0 = base / g.row_chunks;
@@ -89,9 +91,15 @@ hipError_t launch_dropout(int64_t T, int64_t h, const void* x, int64_t ld_x, con
   g.key0 = (uint32_t)seed; g.key1 = (uint32_t)(seed >> 32);
   g.scale = threshold < 65536u ? (float)(65536.0 / (65536.0 - threshold)) : 0.f;
   g.offset = offset; g.offset_dev = offset_dev;
-  const unsigned blocks = (unsigned)((g.n_chunks + DO_THREADS * DO_CHUNKS - 1) / (DO_THREADS * DO_CHUNKS));
-  if (res) hipLaunchKernelGGL(HIP_KERNEL_NAME(dropout_kernel<true>), dim3(blocks), dim3(DO_THREADS), 0, s, g);
-  else hipLaunchKernelGGL(HIP_KERNEL_NAME(dropout_kernel<false>), dim3(blocks), dim3(DO_THREADS), 0, s, g);
+  // four chunks per lane (their loads in flight together) where that leaves every CU two workgroups
+  const auto launch = [&](auto chunks) {
+    constexpr int CHUNKS = decltype(chunks)::value;
+    const dim3 blocks((unsigned)((g.n_chunks + DO_THREADS * CHUNKS - 1) / (DO_THREADS * CHUNKS)));
+    if (res) hipLaunchKernelGGL(HIP_KERNEL_NAME(dropout_kernel<true, CHUNKS>), blocks, dim3(DO_THREADS), 0, s, g);
+    else hipLaunchKernelGGL(HIP_KERNEL_NAME(dropout_kernel<false, CHUNKS>), blocks, dim3(DO_THREADS), 0, s, g);
+  };
+  if (g.n_chunks >= 512 * DO_THREADS * 4) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 

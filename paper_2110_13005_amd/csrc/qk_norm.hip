@@ -275,7 +275,7 @@ static QkPlan qk_plan(int64_t T, int heads, int kv, int d, int rot, bool backwar
   p.tokens = 1;
   while (p.tokens < 8 && p.tokens * std::min(heads, 2 * kv) < 4 * QK_THREADS / p.lph && T >= (p.tokens == 1 ? 64 : 1024 * p.tokens)) p.tokens *= 2;
   const int64_t turns = (T + p.tokens - 1) / p.tokens;
-  int64_t q = turns, k = turns;
+  int64_t q = std::min<int64_t>(turns, 1 << 20), k = q; // a workgroup takes one turn after the other
   if (backward) {                                       // a row of sums per workgroup: shared out by the heads
     q = std::min<int64_t>(turns, std::max<int64_t>(1, (int64_t)QK_BACKWARD_BLOCKS * heads / (heads + 2 * kv)));
     k = std::min<int64_t>(turns, std::max<int64_t>(1, QK_BACKWARD_BLOCKS - q));

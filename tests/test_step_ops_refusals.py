@@ -56,6 +56,7 @@ def test_qk_norm_rope():
         refused(INV, B.axonn_qk_norm_rope_fwd, *with_args(ok, _5=rot))
     for eps in (0.0, -1e-6, float("nan"), float("inf")):
         refused(INV, B.axonn_qk_norm_rope_fwd, *with_args(ok, _11=eps))
+    refused(INV, B.axonn_qk_norm_rope_fwd, *with_args(ok, _13=A + 4))
     refused(INV, B.axonn_qk_norm_rope_fwd, *with_args(ok, _8=127))
     refused(INV, B.axonn_qk_norm_rope_fwd, *with_args(ok, _15=127, _14=2 * A))
     refused(INV, B.axonn_qk_norm_rope_fwd, *with_args(ok, _15=136))                # in place, another leading dimension
