@@ -300,22 +300,6 @@ __device__ __forceinline__ WideFrag widen(intx8 f, float scale) {
 // Columns n .. n + count of row m, count <= 8: v = the sums, bv = their bias.
 template <int EPI>
 __device__ __forceinline__ void fp8_epilogue8(const Fp8Args& g, float (&v)[8], const float (&bv)[8], int m, int n, int count) {
-  if constexpr (EPI == EPI_ACC_F32) {
-    float* p = (float*)g.C + (int64_t)m * g.ldc + n;
-    if (count >= 8) {
-      typedef floatx4 floatx4_any __attribute__((aligned(4)));
-      floatx4_any* pv = (floatx4_any*)p;
-      floatx4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
-      if (g.accumulate) { lo += pv[0]; hi += pv[1]; }
-      pv[0] = lo;
-      pv[1] = hi;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < count) p[e] = v[e] + (g.accumulate ? p[e] : 0.f);
-    }
-    return;
-  }
   elem_t* const c = (elem_t*)g.C + (int64_t)m * g.ldc + n;
   elemx8 x = {}, out;
   if (EPI == EPI_BIAS_RES) x = load_chunk(g.res + (int64_t)m * g.ld_side + n, count);
@@ -345,13 +329,28 @@ __device__ __forceinline__ void fp8_epilogue8(const Fp8Args& g, float (&v)[8], c
   store_chunk(c, out, count);
 }
 
+// The same for 32-bit results, four columns.
+__device__ __forceinline__ void fp8_epilogue4(const Fp8Args& g, floatx4 v, int m, int n, int count) {
+  typedef floatx4 floatx4_any __attribute__((aligned(4)));
+  float* const p = (float*)g.C + (int64_t)m * g.ldc + n;
+  if (count >= 4) {
+    if (g.accumulate) v += *(const floatx4_any*)p;
+    *(floatx4_any*)p = v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < count) p[e] = v[e] + (g.accumulate ? p[e] : 0.f);
+  }
+}
+
 // A wave's TM x TN result tiles at (m0, n0), IP tile rows at a time through `stage`, the wave's own part of LDS
 // (16 * IP rows of 16 * TN floats, 16-byte chunk c of row r at c ^ (r % 8): conflict-free both ways).  Straight from the MFMA's
 // layout an instruction would touch 16 rows with 32 bytes each; from LDS it stores rows of up to 256 bytes.
 template <int EPI, int TM, int TN, int IP>
 __device__ __forceinline__ void fp8_epilogue(const Fp8Args& g, const floatx4 (&acc)[TM][TN], float* stage, int m0, int n0, int lane) {
-  constexpr int LD = 16 * TN, LPR = 2 * TN, RPI = 64 / LPR;          // lanes of a row, rows of an instruction
-  const int n = n0 + 8 * (lane % LPR), count = g.N - n;
+  constexpr int WIDTH = EPI == EPI_ACC_F32 ? 4 : 8;                  // columns of a lane
+  constexpr int LD = 16 * TN, LPR = LD / WIDTH, RPI = 64 / LPR;      // lanes of a row, rows of an instruction
+  const int n = n0 + WIDTH * (lane % LPR), count = g.N - n;
   float bv[8];
   {
     elemx8 b = {};
@@ -369,8 +368,12 @@ __device__ __forceinline__ void fp8_epilogue(const Fp8Args& g, const floatx4 (&a
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int t = 0; t < 16 * IP; t += RPI) {
-      const int row = t + lane / LPR, m = m0 + 16 * i0 + row, c = 2 * (lane % LPR);
+      const int row = t + lane / LPR, m = m0 + 16 * i0 + row, c = WIDTH / 4 * (lane % LPR);
       const float* s = stage + row * LD;
+      if constexpr (EPI == EPI_ACC_F32) {
+        if (m < g.M && count > 0) fp8_epilogue4(g, *reinterpret_cast<const floatx4*>(s + 4 * (c ^ (row & 7))), m, n, count);
+        continue;
+      }
       const floatx4 lo = *reinterpret_cast<const floatx4*>(s + 4 * (c ^ (row & 7)));
       const floatx4 hi = *reinterpret_cast<const floatx4*>(s + 4 * ((c + 1) ^ (row & 7)));
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -751,12 +754,16 @@ static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
   const int64_t t64 = tiles(64, 64), t128 = tiles(128, 128), t256 = tiles(256, 256);
   auto rounds = [](int64_t t, int64_t per) { return (double)((t + per - 1) / per); };
   if constexpr (EPI == EPI_ACC_F32) {
-    // bf16 MFMAs.  Modelled / measured, 64 x 64 and 128 x 128: 512 x 512 x 4096 14 / 14, 32 / 32;  2048^3 25 / 24, 24 / 24;
-    // 2047 x 2048 x 8192 86 / 82, 80 / 75;  2048 x 8192 x 2047 99 / 90, 73 / 73.
-    const double small = rounds(t64, 512) * (2.0 + g.nk * (t64 > 256 ? 0.64 : 0.39));
-    const double big = rounds(t128, 512) * (3.0 + g.nk * (t128 > 256 ? 2.1 : t128 > 128 ? 1.2 : 0.91));
-    if (small < big) return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
-    return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
+    // bf16 MFMAs, with a part for the results' stores.  256 x 256 tiles by eight waves of 128 x 64 convert a code 1.5 times per
+    // matrix instruction, 128 x 128 by four of 64 x 64 twice.  Modelled / measured, 64 x 64, 128 x 128 and 256 x 256:
+    // 512 x 512 x 4096 14 / 15, 32 / 33, 77 / 82;  2048^3 24 / 25, 23 / 23, 45 / 47;  2048 x 8192 x 2047 94 / 91, 65 / 66, 56 / 59;
+    // 1536 x 6144 x 8192 212 / 172, 223 / 156, 166 / 160;  8192^3 on the last two 893 / 850, 722 / 733 (1500 TFLOP/s).
+    const double small = rounds(t64, 512) * (1.5 + g.nk * (t64 > 256 ? 0.64 : 0.39));
+    const double mid = rounds(t128, 512) * (2.5 + 3.5 * std::min(1.0, t128 / 512.0) + g.nk * (t128 > 256 ? 1.65 : t128 > 128 ? 1.2 : 0.91));
+    const double big = rounds(t256, 256) * (6.0 + 8.0 * std::min(1.0, t256 / 256.0) + g.nk * (2.2 + 0.4 * std::min(1.0, t256 / 256.0)));
+    if (big < mid && big < small) return launch_fp8_tile<2, 4, 8, 4, 2, EPI>(g, s);
+    if (mid < small) return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
+    return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
   } else {
     const double small = rounds(t64, 512) * (1.8 + g.nk * (t64 > 256 ? 0.40 : 0.22));
     const double mid = rounds(t128, 256) * (2.3 + g.nk * (t128 > 128 ? 0.55 : 0.45));
