@@ -384,9 +384,9 @@ __device__ __forceinline__ void fp8_epilogue(const Fp8Args& g, const floatx4 (&a
 }
 
 // Tile of a workgroup: contiguous runs of tiles for each XCD (workgroups go round the eight), in bands of 8 tile rows.
-__device__ __forceinline__ void fp8_tile_at(int pid, int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int band_tiles = 8 * tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
-  const int rows = min(8, tiles_m - band * 8);
+__device__ __forceinline__ void fp8_tile_at(const Fp8Args& g, int pid, int& tm, int& tn) {
+  const int band_tiles = 8 * g.tiles_n, band = pid / band_tiles, in_band = pid - band * band_tiles;
+  const int rows = min(8, g.tiles_m - band * 8);
   tm = band * 8 + in_band % rows;
   tn = in_band / rows;
 }
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_kernel(const Fp8Args g)
   const int wm = wave / WN, wn = wave % WN;
   int pid = blockIdx.x, tm, tn;
   if ((gridDim.x & 7) == 0) pid = (pid & 7) * (gridDim.x >> 3) + (pid >> 3);
-  fp8_tile_at(pid, g.tiles_m, g.tiles_n, tm, tn);
+  fp8_tile_at(g, pid, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const uint32_t Kp = (uint32_t)g.Kp, S = (uint32_t)g.S;
   const uint32_t live_m = min(BM, g.M - m0), live_n = min(BN, g.N - n0);
@@ -515,6 +515,114 @@ __global__ __launch_bounds__(64 * WM * WN) void gemm_fp8_kernel(const Fp8Args g)
   fp8_epilogue<EPI, TM, TN, IP>(g, acc, (float*)smem + wave * (16 * IP * 16 * TN), m0 + wm * TM * 16, n0 + wn * TN * 16, lane);
 }
 
+// 128 x 128 tiles, four waves, one per SIMD, each 64 x 64 of the result: what has too few tiles for the next kernel.  LDS bounds it:
+// 64 KB of fragments and 32 KB of copies per tile of k, 768 cycles of the 850 to 1050 that it takes, to 512 of MFMAs.  Eight waves of
+// 64 x 32 read 96 KB: 2047 x 2048 x 8192 in 38 us, this way 32 (2110 TFLOP/s).  While
+// the MFMAs of a tile of k run from registers, the next one's fragments are read and the one three ahead is copied to where
+// the tile before lay, whose fragments every wave has in registers at the barrier.
+template <int EPI>
+__global__ __launch_bounds__(256) void gemm_fp8_mid_kernel(const Fp8Args g) {
+  constexpr int BM = 128, BN = 128, STAGE = (BM + BN) * FB, SCALES = 4 * STAGE, SBUF = (BM + BN) * 4;
+  __shared__ __align__(1024) char smem[SCALES + 2 * SBUF];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  int pid = blockIdx.x, tm, tn;
+  if ((gridDim.x & 7) == 0) pid = (pid & 7) * (gridDim.x >> 3) + (pid >> 3);
+  fp8_tile_at(g, pid, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  const uint32_t Kp = (uint32_t)g.Kp, S = (uint32_t)g.S;
+  const uint32_t live_m = min(BM, g.M - m0), live_n = min(BN, g.N - n0);
+  const u32x4 ra = rsrc_words(g.A + (int64_t)m0 * g.Kp, live_m * Kp), rb = rsrc_words(g.B + (int64_t)n0 * g.Kp, live_n * Kp);
+  const u32x4 rs = wave < 2 ? rsrc_words(g.sa + (int64_t)m0 * g.S, live_m * S) : rsrc_words(g.sb + (int64_t)n0 * g.S, live_n * S);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(AXONN_LDS char*)smem;
+  const uint32_t at_lane = (uint32_t)(8 * wave + (lane >> 3)) * Kp + 16u * ((lane & 7) ^ (lane >> 3));
+  const uint32_t scale_lane = (uint32_t)((wave & 1) * 64 + lane) * S;
+  // copy c of 0..7 of tile kt into `slot`: 8 rows of A, then of B, per wave
+  auto copy = [&](int kt, int slot, int c) {
+    dma_chunk16(c < 4 ? ra : rb, at_lane + (uint32_t)(32 * (c & 3)) * Kp, kt < g.nk ? (uint32_t)kt * FB : 0,
+                lds0 + slot * STAGE + wave * 1024 + c * 4096);
+  };
+  auto copy_scales = [&](int kt) {                       // of tiles kt .. kt + 3
+    if (kt < g.nk) dma_word(rs, scale_lane, kt, lds0 + SCALES + (kt >> 2 & 1) * SBUF + wave * 256);
+  };
+  const int r = lane & 15, q = lane >> 4;
+  const int f[2] = {r * FB + 16 * (q ^ (r & 7)), r * FB + 16 * ((q + 4) ^ (r & 7))};
+  const char* const a_of = smem + wm * (64 * FB);
+  const char* const b_of = smem + BM * FB + wn * (64 * FB);
+  union Frag { intx8 v; u32x4 h[2]; };
+  Frag fa[2][4], fb[2][4];
+  int sa[4], sb[4], sa_next[4] = {}, sb_next[4] = {};
+  // half x & 1 of fragment x / 2 of a tile, in the order of their use: A 0, B 0 to 3, A 1 to 3
+  auto read = [&](int set, int slot, int x) {
+    const int n = x >> 1, h = x & 1;
+    if (n == 0 || n > 4) {
+      const int i = n == 0 ? 0 : n - 4;
+      fa[set][i].h[h] = *reinterpret_cast<const u32x4*>(a_of + slot * STAGE + i * 16 * FB + f[h]);
+    } else {
+      fb[set][n - 1].h[h] = *reinterpret_cast<const u32x4*>(b_of + slot * STAGE + (n - 1) * 16 * FB + f[h]);
+    }
+  };
+  auto read_scale = [&](int kt, int (&a)[4], int (&b)[4], int x) {
+    const int* s = reinterpret_cast<const int*>(smem + SCALES + (kt >> 2 & 1) * SBUF) + r;
+    if (x < 4) a[x] = s[wm * 64 + 16 * x];
+    else b[x - 4] = s[BM + wn * 64 + 16 * (x - 4)];
+  };
+  floatx4 acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  copy_scales(0);
+#pragma unroll
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) copy(i, i, c);
+  asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+  lds_barrier();
+#pragma unroll
+  for (int x = 0; x < 16; ++x) read(0, 0, x);
+#pragma unroll
+  for (int x = 0; x < 8; ++x) read_scale(0, sa, sb, x);
+  auto step = [&](auto byte, int kt) {
+    constexpr int J = decltype(byte)::value, P = J & 1;
+    asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
+    if (J == 0) copy_scales(kt + 4);
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const int i = x >> 2, j = x & 3;
+      acc[i][j] = mfma_fp8<J>(fb[P][j].v, fa[P][i].v, acc[i][j], sb[j], sa[i]);
+      if (x < 8) {
+        read(P ^ 1, (J + 1) & 3, 2 * x);
+        read(P ^ 1, (J + 1) & 3, 2 * x + 1);
+      }
+      if (x & 1) copy(kt + 3, (J + 3) & 3, x >> 1);
+      if (J == 3 && x < 8) read_scale(kt + 1, sa_next, sb_next, x);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if (J == 3) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        sa[i] = sa_next[i];
+        sb[i] = sb_next[i];
+      }
+    }
+  };
+  using std::integral_constant;
+  int kt = 0;
+  for (; kt + 4 <= g.nk; kt += 4) {
+    step(integral_constant<int, 0>{}, kt);
+    step(integral_constant<int, 1>{}, kt + 1);
+    step(integral_constant<int, 2>{}, kt + 2);
+    step(integral_constant<int, 3>{}, kt + 3);
+  }
+  if (kt < g.nk) step(integral_constant<int, 0>{}, kt);
+  if (kt + 1 < g.nk) step(integral_constant<int, 1>{}, kt + 1);
+  if (kt + 2 < g.nk) step(integral_constant<int, 2>{}, kt + 2);
+  dma_wait_all();                                        // copies of tiles past the end still write to LDS
+  lds_barrier();
+  fp8_epilogue<EPI, 4, 4, 2>(g, acc, (float*)smem + wave * (16 * 2 * 64), m0 + wm * 64, n0 + wn * 64, lane);
+}
+
 // The product for problems that fill the chip with 256 x 256 tiles: four waves, one per SIMD, each 128 x 128 of the result, the
 // 256 accumulators in the accumulation registers.  With 8 waves of 128 x 64 (196 KB of fragments per tile of k instead of 128 KB,
 // and every wave at the barrier with nothing to do) the product of 8192 x 5120 x 20480 took 1000 us, this way 725 (2370 TFLOP/s;
@@ -558,7 +666,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
     Tile t = {g.M, g.N};
     if (p < end) {
       int tm, tn;
-      fp8_tile_at(p, g.tiles_m, g.tiles_n, tm, tn);
+      fp8_tile_at(g, p, tm, tn);
       t.m0 = __builtin_amdgcn_readfirstlane(tm * BM);
       t.n0 = __builtin_amdgcn_readfirstlane(tn * BN);
     }
@@ -727,27 +835,34 @@ __global__ __launch_bounds__(256) void gemm_fp8_big_kernel(const Fp8Args g) {
 #undef AXONN_AS_LOADED
 }
 
+static void fp8_tiles(Fp8Args& g, int bm, int bn) {
+  g.tiles_m = (g.M + bm - 1) / bm;
+  g.tiles_n = (g.N + bn - 1) / bn;
+}
 template <int WM, int WN, int TM, int TN, int NS, int EPI>
 static hipError_t launch_fp8_tile(Fp8Args g, hipStream_t s) {
-  constexpr int BM = WM * TM * 16, BN = WN * TN * 16;
-  g.tiles_m = (g.M + BM - 1) / BM;
-  g.tiles_n = (g.N + BN - 1) / BN;
+  fp8_tiles(g, WM * TM * 16, WN * TN * 16);
   hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_kernel<WM, WN, TM, TN, NS, EPI>), dim3((unsigned)(g.tiles_m * g.tiles_n)),
                      dim3(64 * WM * WN), 0, s, g);
   return hipGetLastError();
 }
 template <int EPI>
+static hipError_t launch_fp8_mid(Fp8Args g, hipStream_t s) {
+  fp8_tiles(g, 128, 128);
+  hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_mid_kernel<EPI>), dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(256), 0, s, g);
+  return hipGetLastError();
+}
+template <int EPI>
 static hipError_t launch_fp8_big(Fp8Args g, hipStream_t s) {
-  g.tiles_m = (g.M + 255) / 256;
-  g.tiles_n = (g.N + 255) / 256;
+  fp8_tiles(g, 256, 256);
   hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_big_kernel<EPI>), dim3((unsigned)std::min(256, g.tiles_m * g.tiles_n)), dim3(256), 0, s, g);
   return hipGetLastError();
 }
 // The kernel with the least modelled time: rounds of workgroups, each a fixed part and a part per 128 of k, in us.  The parts are
-// from single launches of outputs of 512 x 512 to 8192 x 20480 with K = 512 to 8192; a CU that is shared is slower per step.
-// Modelled / measured, 64 x 64, 128 x 128 and 256 x 256: 512 x 512 x 4096 8.8 / 8.8, 16.7 / 16.3, 43 / 42;  2048^3 16.4 / 15.7,
-// 11.1 / 12.1, 27 / 27;  2047 x 2048 x 8192 55 / 53, 37 / 38, 81 / 78;  2048 x 6144 x 2048 (two thirds of the CUs for the
-// last) 33 / 45, 33 / 34, 30 / 30;  4096^3 117 / 102, 80 / 78, 52 / 55.
+// from single launches of outputs of 200 x 392 to 8192 x 20480 with K = 512 to 16384; a CU that is shared is slower per step.
+// Modelled / measured, 64 x 64, 128 x 128 and 256 x 256: 512 x 512 x 4096 8.8 / 8.9, 14 / 13, 43 / 42;  2048^3 17 / 16,
+// 9.4 / 10.9, 27 / 27;  2047 x 2048 x 8192 57 / 57, 31 / 32, 80 / 78;  2048 x 6144 x 2048 (two thirds of the CUs for the
+// last) 51 / 44, 28 / 31, 29 / 31;  4096^3 122 / 101, 67 / 70, 52 / 55.
 template <int EPI>
 static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
   auto tiles = [&](int64_t bm, int64_t bn) { return (g.M + bm - 1) / bm * ((g.N + bn - 1) / bn); };
@@ -765,11 +880,11 @@ static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
     if (mid < small) return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
     return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
   } else {
-    const double small = rounds(t64, 512) * (1.8 + g.nk * (t64 > 256 ? 0.40 : 0.22));
-    const double mid = rounds(t128, 256) * (2.3 + g.nk * (t128 > 128 ? 0.55 : 0.45));
+    const double small = rounds(t64, 512) * (1.8 + g.nk * (t64 > 256 ? 0.42 : 0.22));
+    const double mid = rounds(t128, 256) * (2.0 + g.nk * (0.37 + 0.09 * std::min(1.0, t128 / 256.0)));
     const double big = 4.0 + rounds(t256, 256) * (5.0 + (g.nk + 3) / 4 * 4 * (1.05 + 0.3 * std::min(1.0, t256 / 256.0)));
     if (big < mid && big < small) return launch_fp8_big<EPI>(g, s);
-    if (mid < small) return launch_fp8_tile<2, 4, 4, 2, 4, EPI>(g, s);
+    if (mid < small) return launch_fp8_mid<EPI>(g, s);
     return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
   }
 }
