@@ -2,7 +2,7 @@
 //
 //   out[t, :] = scale * table[id_t, :]            dtable[v, :] (+)= scale * sum over the tokens t with id_t = v of dout[t, :]
 //
-// Both are bound by HBM.  The gradient's sums are formed in fp32 in the order of the tokens (a stable sort of the ids, then
+// Both are bound by HBM.  The gradient's sums are formed in fp32 in the order of the tokens (equal ids brought together in the tokens' order, then
 // fixed pieces of the sorted list, then the pieces of one id in order): no atomics on values, the same bits every run.
 // Ids outside [0, vocab) are clamped into range, as everywhere in the library.
 #include "rows.h"
@@ -171,12 +171,15 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_scatter_kernel(co
   }
 }
 
-// Up to SORT_RANGE_MAX tokens in one launch: a workgroup per range of ids looks at all tokens, counts those below its range (its
-// place in the list) and sorts those in it, in LDS: id and token index as one 32-bit key, one pass per digit as in the scatter
-// kernel, none if they are all the same.  The launch's other workgroups clear the table meanwhile.  A workgroup that sorted
-// all ids by itself was bound by its ballots: 30 us for 16384 tokens.
-constexpr int SORT_RANGE_THREADS = 1024, SORT_RANGE_WAVES = SORT_RANGE_THREADS / 64, SORT_RANGE_ITEMS = 16;
-constexpr int SORT_RANGE_MAX = SORT_RANGE_THREADS * SORT_RANGE_ITEMS, SORT_RANGE_BITS = 8, SORT_RANGES = 32;
+// Up to SORT_SHARE_MAX tokens in one launch, and equal ids only brought together: a workgroup per residue of the ids modulo
+// SORT_SHARES looks at all tokens, counts those of smaller residues (its place in the list) and sorts its own, in LDS: quotient
+// and token index as one 32-bit key, one pass per digit as in the scatter kernel, none if they are all the same.  The launch's
+// other workgroups clear the table meanwhile.  A workgroup that sorted all ids by itself was bound by its ballots: 30 us for 16384
+// tokens; with ranges of consecutive ids the one of a text's most frequent words had
+// most of them.
+constexpr int SORT_SHARE_THREADS = 1024, SORT_SHARE_WAVES = SORT_SHARE_THREADS / 64, SORT_SHARE_ITEMS = 16;
+constexpr int SORT_SHARE_MAX = SORT_SHARE_THREADS * SORT_SHARE_ITEMS, SORT_SHARE_BITS = 8;
+constexpr int SORT_SHARES_LOG = 5, SORT_SHARES = 1 << SORT_SHARES_LOG;
 
 // Zeros to `halves` 16-bit numbers from p on, by workgroup `block` of `blocks`: four chunks per thread and round.
 template <int THREADS>
@@ -197,32 +200,33 @@ __device__ __forceinline__ void clear_table(uint16_t* p, int64_t halves, int64_t
   }
 }
 
-__global__ __launch_bounds__(SORT_RANGE_THREADS) void embedding_sort_range_kernel(int T, int vocab, int range_bits, int ranges, int t_bits,
+__global__ __launch_bounds__(SORT_SHARE_THREADS) void embedding_sort_share_kernel(int T, int vocab, int key_bits, int shares, int t_bits,
                                                                                   const int* __restrict__ tokens, int* __restrict__ ids,
                                                                                   int* __restrict__ order, uint16_t* clear, int64_t halves) {
-  constexpr int BINS = 1 << SORT_RANGE_BITS;
-  __shared__ uint32_t list[SORT_RANGE_MAX];
-  __shared__ uint32_t counter[SORT_RANGE_WAVES][BINS];
-  __shared__ uint32_t wave_sum[SORT_RANGE_WAVES], wave_below[SORT_RANGE_WAVES];
-  if ((int)blockIdx.x >= ranges) {
-    clear_table<SORT_RANGE_THREADS>(clear, halves, blockIdx.x - ranges, gridDim.x - ranges);
+  constexpr int BINS = 1 << SORT_SHARE_BITS;
+  __shared__ uint32_t list[SORT_SHARE_MAX];
+  __shared__ uint32_t counter[SORT_SHARE_WAVES][BINS];
+  __shared__ uint32_t wave_sum[SORT_SHARE_WAVES], wave_below[SORT_SHARE_WAVES];
+  if ((int)blockIdx.x >= shares) {
+    clear_table<SORT_SHARE_THREADS>(clear, halves, blockIdx.x - shares, gridDim.x - shares);
     return;
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t range = blockIdx.x;
-  // the tokens of this range, in order: wave w looks at 64 * looks consecutive ones
-  const int looks = (T + SORT_RANGE_THREADS - 1) / SORT_RANGE_THREADS;
-  int id[SORT_RANGE_ITEMS];
+  const int share = blockIdx.x;
+  auto share_of = [](int id) { return id & (SORT_SHARES - 1); };
+  // the tokens of this share, in order: wave w looks at 64 * looks consecutive ones
+  const int looks = (T + SORT_SHARE_THREADS - 1) / SORT_SHARE_THREADS;
+  int id[SORT_SHARE_ITEMS];
   uint32_t taken = 0, below = 0;
 #pragma unroll
-  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+  for (int k = 0; k < SORT_SHARE_ITEMS; ++k) {
     const int i = (wave * looks + k) * 64 + lane;
-    id[k] = k < looks && i < T ? clamp_token(tokens[i], vocab) : 0x7fffffff;
+    id[k] = k < looks && i < T ? clamp_token(tokens[i], vocab) : -1;
   }
 #pragma unroll
-  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
-    taken += __popcll(__ballot((uint32_t)id[k] >> range_bits == range));
-    below += __popcll(__ballot((uint32_t)id[k] >> range_bits < range));
+  for (int k = 0; k < SORT_SHARE_ITEMS; ++k) {
+    taken += __popcll(__ballot(id[k] >= 0 && share_of(id[k]) == share));
+    below += __popcll(__ballot(id[k] >= 0 && share_of(id[k]) < share));
   }
   if (lane == 0) {
     wave_sum[wave] = taken;
@@ -230,39 +234,39 @@ __global__ __launch_bounds__(SORT_RANGE_THREADS) void embedding_sort_range_kerne
   }
   __syncthreads();
   uint32_t at = 0, n = 0, base = 0;
-  for (int w = 0; w < SORT_RANGE_WAVES; ++w) {
+  for (int w = 0; w < SORT_SHARE_WAVES; ++w) {
     if (w < wave) at += wave_sum[w];
     n += wave_sum[w];
     base += wave_below[w];
   }
   if (n == 0) return;
 #pragma unroll
-  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
-    const bool in = (uint32_t)id[k] >> range_bits == range;
+  for (int k = 0; k < SORT_SHARE_ITEMS; ++k) {
+    const bool in = id[k] >= 0 && share_of(id[k]) == share;
     const unsigned long long m = __ballot(in);
-    if (in) list[at + __popcll(m & ((1ull << lane) - 1))] = (uint32_t)id[k] << t_bits | (uint32_t)((wave * looks + k) * 64 + lane);
+    if (in) list[at + __popcll(m & ((1ull << lane) - 1))] = (uint32_t)id[k] >> SORT_SHARES_LOG << t_bits | (uint32_t)((wave * looks + k) * 64 + lane);
     at += __popcll(m);
   }
   __syncthreads();
   // sort list[0 .. n): wave w owns 64 * items consecutive places
-  const int items = ((int)n + SORT_RANGE_THREADS - 1) / SORT_RANGE_THREADS, first = wave * 64 * items + lane;
-  uint32_t key[SORT_RANGE_ITEMS], rank[SORT_RANGE_ITEMS];
+  const int items = ((int)n + SORT_SHARE_THREADS - 1) / SORT_SHARE_THREADS, first = wave * 64 * items + lane;
+  uint32_t key[SORT_SHARE_ITEMS], rank[SORT_SHARE_ITEMS];
   bool other = false;
   const uint32_t some = list[0] >> t_bits;
 #pragma unroll
-  for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+  for (int k = 0; k < SORT_SHARE_ITEMS; ++k) {
     const int i = first + 64 * k;
     key[k] = k < items && i < (int)n ? list[i] : 0;
     other |= k < items && i < (int)n && key[k] >> t_bits != some;
   }
   const bool unsorted = __syncthreads_or(other);
-  for (int shift = 0; unsorted && shift < range_bits; shift += SORT_RANGE_BITS) {
-    const int digit_bits = min(SORT_RANGE_BITS, range_bits - shift), low = t_bits + shift;
-    for (int b = tid; b < SORT_RANGE_WAVES * BINS; b += SORT_RANGE_THREADS) (&counter[0][0])[b] = 0;
+  for (int shift = 0; unsorted && shift < key_bits; shift += SORT_SHARE_BITS) {
+    const int digit_bits = min(SORT_SHARE_BITS, key_bits - shift), low = t_bits + shift;
+    for (int b = tid; b < SORT_SHARE_WAVES * BINS; b += SORT_SHARE_THREADS) (&counter[0][0])[b] = 0;
     __syncthreads();
     volatile uint32_t* const mine = counter[wave];
 #pragma unroll
-    for (int k = 0; k < SORT_RANGE_ITEMS; ++k) {
+    for (int k = 0; k < SORT_SHARE_ITEMS; ++k) {
       if (k >= items) continue;
       const bool live = first + 64 * k < (int)n;
       const uint32_t digit = key[k] >> low & ((1u << digit_bits) - 1);
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(SORT_RANGE_THREADS) void embedding_sort_range_kerne
     // counters -> places: exclusive over the digits, then over the waves
     uint32_t total = 0, scan = 0;
     if (wave < BINS / 64) {
-      for (int w = 0; w < SORT_RANGE_WAVES; ++w) total += counter[w][tid];
+      for (int w = 0; w < SORT_SHARE_WAVES; ++w) total += counter[w][tid];
       scan = total;
       for (int o = 1; o < 64; o <<= 1) {
         const uint32_t up = __shfl_up(scan, o, 64);
@@ -294,7 +298,7 @@ __global__ __launch_bounds__(SORT_RANGE_THREADS) void embedding_sort_range_kerne
     if (wave < BINS / 64) {
       uint32_t place = scan - total;
       for (int w = 0; w < wave; ++w) place += wave_sum[w];
-      for (int w = 0; w < SORT_RANGE_WAVES; ++w) {
+      for (int w = 0; w < SORT_SHARE_WAVES; ++w) {
         const uint32_t c = counter[w][tid];
         counter[w][tid] = place;
         place += c;
@@ -302,26 +306,26 @@ __global__ __launch_bounds__(SORT_RANGE_THREADS) void embedding_sort_range_kerne
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < SORT_RANGE_ITEMS; ++k)
+    for (int k = 0; k < SORT_SHARE_ITEMS; ++k)
       if (k < items && first + 64 * k < (int)n) list[mine[key[k] >> low & ((1u << digit_bits) - 1)] + rank[k]] = key[k];
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < SORT_RANGE_ITEMS; ++k)
+    for (int k = 0; k < SORT_SHARE_ITEMS; ++k)
       if (k < items && first + 64 * k < (int)n) key[k] = list[first + 64 * k];
   }
 #pragma unroll
-  for (int k = 0; k < SORT_RANGE_ITEMS; ++k)
+  for (int k = 0; k < SORT_SHARE_ITEMS; ++k)
     if (k < items && first + 64 * k < (int)n) {
-      ids[base + first + 64 * k] = (int)(key[k] >> t_bits);
+      ids[base + first + 64 * k] = (int)(key[k] >> t_bits << SORT_SHARES_LOG) | share;
       order[base + first + 64 * k] = (int)(key[k] & ((1u << t_bits) - 1));
     }
 }
 
 // --------------------------------------------------------------------------------------------------------------- sums
 // The sorted list is cut into pieces; a wave adds the rows of one piece over 512 columns (8 per lane), SUM_BATCH of them in
-// flight.  Pieces are one batch, or four where there are many tokens: fewer sums of runs that cross pieces.  A run of equal ids that lies within the piece is finished here; one that crosses the piece's start
-// leaves its sum in partial[piece][0], one that begins in the piece and crosses its end in partial[piece][1], and
-// embedding_bwd_join_kernel adds them up.
+// flight.  Pieces are one batch, or four where there are many tokens: fewer sums of runs that cross pieces.  A run of equal ids
+// that lies within the piece is finished here; one that crosses the piece's start leaves its sum in partial[piece][0], one that
+// begins in the piece and crosses its end in partial[piece][1], and embedding_bwd_join_kernel adds them up.
 constexpr int SUM_BATCH = 16, SUM_COLS = 512;
 constexpr int PIECE_FEW = SUM_BATCH, PIECE_MANY = 4 * SUM_BATCH, MANY_TOKENS = 32768;
 typedef floatx4 floatx4_any __attribute__((aligned(4)));
@@ -339,8 +343,7 @@ struct TableGrad {
 
 // Columns c .. c + n of row id, n of 8 (8 or more: all).
 template <bool FP32>
-__device__ __forceinline__ void store_table_row(const TableGrad& g, int id, int c, int n, const float (&acc)[8]) {
-  const float scale = g.scale;
+__device__ __forceinline__ void store_table_row(const TableGrad& g, int id, int c, int n, const float (&acc)[8], float scale) {
   const bool accumulate = g.accumulate;
   if constexpr (FP32) {
     float* p = (float*)g.dtable + (int64_t)id * g.h + c;
@@ -414,7 +417,7 @@ __global__ __launch_bounds__(256) void embedding_bwd_sum_kernel(const TableGrad 
         if (next != cur || final) {
           const bool head = from_start && before == cur, tail = next == cur;
           if (n > 0) {
-            if (!head && !tail) store_table_row<FP32>(g, cur, c, n, acc);
+            if (!head && !tail) store_table_row<FP32>(g, cur, c, n, acc, g.scale);
             else {
               float* p = g.partial + ((int64_t)piece * 2 + (head ? 0 : 1)) * g.h + c;
               if (n >= 8) {
@@ -498,7 +501,7 @@ __global__ __launch_bounds__(256) void embedding_bwd_join_kernel(const TableGrad
   for (int w = 0; w < 3; ++w)
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] += sums[w][lane][e];
-  store_table_row<FP32>(g, id, c, n, acc);
+  store_table_row<FP32>(g, id, c, n, acc, g.scale);
 }
 
 // Up to FEW_MAX tokens: no sort, and every row of the result has one writer.  A workgroup takes ROWS rows and 512 columns, marks
@@ -588,7 +591,7 @@ __global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const TableGrad 
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] += sums[w][lane][e];
     }
-    if (n > 0) store_table_row<FP32>(g, id, c, n, acc);
+    if (n > 0) store_table_row<FP32>(g, id, c, n, acc, tokens ? g.scale : 0.f);      // no tokens: zeros, whatever the scale
   }
 }
 
@@ -648,13 +651,12 @@ static hipError_t launch_embedding_bwd_t(TableGrad g, const EmbeddingWs& w, cons
   }
   int t_bits = 1;
   while (((int64_t)1 << t_bits) < T) ++t_bits;
-  if (T <= SORT_RANGE_MAX && w.bits + t_bits <= 32) {
-    int range_bits = 0;                                 // the fewest with which SORT_RANGES ranges cover the ids
-    while ((int64_t)SORT_RANGES << range_bits < g.vocab) ++range_bits;
-    const int ranges = (int)((((int64_t)g.vocab - 1) >> range_bits) + 1);
+  const int key_bits = std::max(0, w.bits - SORT_SHARES_LOG);
+  if (T <= SORT_SHARE_MAX && key_bits + t_bits <= 32) {
+    const int shares = std::min(SORT_SHARES, g.vocab);
     const int64_t clearing = g.accumulate ? 0 : std::min<int64_t>(1 << 20, (halves + 32767) / 32768);
-    hipLaunchKernelGGL(embedding_sort_range_kernel, dim3((unsigned)(ranges + clearing)), dim3(SORT_RANGE_THREADS), 0, s, g.T, g.vocab, range_bits,
-                       ranges, t_bits, tokens, (int*)(ws + w.keys[0]), (int*)(ws + w.index[0]), (uint16_t*)g.dtable, halves);
+    hipLaunchKernelGGL(embedding_sort_share_kernel, dim3((unsigned)(shares + clearing)), dim3(SORT_SHARE_THREADS), 0, s, g.T, g.vocab, key_bits,
+                       shares, t_bits, tokens, (int*)(ws + w.keys[0]), (int*)(ws + w.index[0]), (uint16_t*)g.dtable, halves);
     g.ids = (const int*)(ws + w.keys[0]); g.order = (const int*)(ws + w.index[0]);
   } else {
     if (!g.accumulate) clear();

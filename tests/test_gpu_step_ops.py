@@ -127,6 +127,27 @@ def test_embedding_gradient(T, h, V, how, fp32, ld, shift):
         old = got
 
 
+@pytest.mark.parametrize("T,V", [(5, 40), (5, 4000), (300, 4000), (17000, 300)])
+def test_embedding_gradient_of_nan_and_infinity(T, V):
+    """What is not a number in one token's gradient stays in its row, and rows without tokens are zeros whatever the scale."""
+    import torch
+    rng, h = np.random.default_rng(T), 72
+    tokens = rng.integers(0, V // 2, T)
+    dout = normal(rng, T, h)
+    dout[T // 2] = np.nan
+    named, hit = np.unique(tokens), tokens[T // 2]
+    ws = workspace(B.axonn_embedding_bwd_workspace(T, h, V))
+    for scale in (1.0, np.inf):
+        for dt in (B.torch_elem_dtype(), torch.float32):
+            out, x = Padded(V, h, dtype=dt), Padded(T, h, values=dout)
+            B.axonn_embedding_bwd(T, h, V, dev_i32(tokens), x.t, h, scale, out.t, int(dt == torch.float32), 0, ws)
+            got = out.result()
+            assert np.isnan(got[hit]).all()
+            assert not np.delete(got, named, axis=0).any()
+            if scale == 1.0:
+                assert np.isfinite(np.delete(got, hit, axis=0)).all()
+
+
 # ------------------------------------------------------------------------------------- norms of queries and keys, rotation
 def _qk_case(rng, T, heads, kv, d, rot, positions, big=False):
     width = (heads + 2 * kv) * d
