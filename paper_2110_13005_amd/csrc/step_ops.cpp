@@ -170,6 +170,9 @@ int axonn_gemm_fp8(int32_t epilogue, int64_t M, int64_t N, int64_t K, const void
   if (epilogue == EPI_BIAS_RES && (!res || ld_res < N)) return fail_entry(AXONN_EINVAL, "gemm_fp8: epilogue 1 needs res with ld_res >= N");
   if ((epilogue == EPI_BIAS_GELU || epilogue == EPI_DGELU) && (!aux || ld_aux < N))
     return fail_entry(AXONN_EINVAL, "gemm_fp8: epilogue %d needs aux with ld_aux >= N", epilogue);
+  if ((epilogue == EPI_BIAS_RES && C == res && ldc != ld_res) || (epilogue == EPI_DGELU && C == aux && ldc != ld_aux))
+    return fail_entry(AXONN_EINVAL, "gemm_fp8: in place with two leading dimensions");
+  if (epilogue == EPI_BIAS_GELU && C == aux) return fail_entry(AXONN_EINVAL, "gemm_fp8: two results in one place");
   if ((uintptr_t)A % 16 || (uintptr_t)B % 16 || (uintptr_t)a_scale % 4 || (uintptr_t)b_scale % 4)
     return fail_entry(AXONN_EINVAL, "gemm_fp8: codes must be 16-byte aligned, scales 4-byte aligned");
   if (epilogue == EPI_ACC_F32 && (uintptr_t)C % 4) return fail_entry(AXONN_EINVAL, "gemm_fp8: a 32-bit result must be 4-byte aligned");

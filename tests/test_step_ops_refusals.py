@@ -125,6 +125,9 @@ def test_fp8():
     refused(INV, B.axonn_gemm_fp8, *with_args(ok, _4=A + 8))
     refused(INV, B.axonn_gemm_fp8, *with_args(ok, _7=A + 2))
     refused(INV, B.axonn_gemm_fp8, *with_args(ok, _0=B.EPI_ACC_F32, _8=A + 2))
+    refused(INV, B.axonn_gemm_fp8, *with_args(ok, _0=B.EPI_BIAS_RES), res=A, ld_res=24)              # the result over its residual
+    refused(INV, B.axonn_gemm_fp8, *with_args(ok, _0=B.EPI_DGELU), aux=A, ld_aux=24)
+    refused(INV, B.axonn_gemm_fp8, *with_args(ok, _0=B.EPI_BIAS_GELU), aux=A, ld_aux=16)
     refused(UNS, B.axonn_gemm_fp8, *with_args(ok, _3=(1 << 22) + 1))
     refused(UNS, B.axonn_gemm_fp8, *with_args(ok, _1=1 << 20, _2=1 << 20, _9=1 << 20))
 
