@@ -95,11 +95,16 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
-// cos and sin of the angles of `count` tokens from t0 on, [token][pairs], pairs = rot / 2 rounded up to whole chunks.
+// cos and sin of the angles of `count` tokens from t0 on, [token][pairs], pairs = rot / 2 rounded up to whole chunks.  The places behind
+// rot / 2 are no pair's, but a lane with fewer than 8 pairs turns zeros by them, and those take part in the head's sums: they
+// get no rotation, as what LDS holds may be an infinity or NaN.
 __device__ __forceinline__ void qk_angles(const QkArgs& g, int t0, int count, int pairs, float2* cs) {
   for (int i = threadIdx.x; i < count * pairs; i += QK_THREADS) {
     const int k = i / pairs, p = i - k * pairs, t = t0 + k;
-    if (p >= g.rot / 2) continue;
+    if (p >= g.rot / 2) {
+      cs[i] = make_float2(1.f, 0.f);
+      continue;
+    }
     const int pos = g.positions ? g.positions[t] : t % g.seq;
     const double turns = (double)pos * (g.inv_freq[p] * 0.15915494309189533577);       // 1 / (2 pi)
     float s, c;
