@@ -501,6 +501,7 @@ int axonn_embedding_bwd(int64_t T, int64_t h, int64_t vocab, const int32_t* toke
  * the layout axonn_attention_fwd reads).  Every query and key head x of a token is normalised and
  * rotated, V is copied:
  *   z = gamma * x / sqrt(mean(x^2) + eps)              gamma_q, gamma_k: [head_dim] each
+ * (for every finite x and eps, also where the squares alone would overflow or vanish in 32 bits)
  *   (z_a, z_b) -> (z_a cos - z_b sin, z_a sin + z_b cos),  angle = position * inv_freq[i]
  * for the pairs i < rotary_dim / 2: (a, b) = (i, i + rotary_dim / 2), or (2i, 2i + 1) if
  * interleaved; elements from rotary_dim on are not rotated.  The position of token t is

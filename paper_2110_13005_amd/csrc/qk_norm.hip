@@ -95,6 +95,13 @@ __device__ __forceinline__ float head_sum(float v) {
   return v;
 }
 
+// Mean squares plus eps that 32 bits hold with room on both sides.  A head beyond them (bfloat16 values go to 2^128 and down to 2^-133,
+// so their squares may overflow or vanish) is multiplied by 2^-70 or 2^70, which is exact, and with it eps by the square:
+// x / sqrt(mean x^2 + eps) stays what it is.
+constexpr float QK_LEAST = 0x1p-100f, QK_MOST = 0x1p100f;
+__device__ __forceinline__ bool qk_out_of_range(float v) { return v < QK_LEAST || v > QK_MOST; }
+__device__ __forceinline__ float qk_range_scale(float v) { return v > QK_MOST ? 0x1p-70f : v < QK_LEAST ? 0x1p70f : 1.f; }
+
 // cos and sin of the angles of `count` tokens from t0 on, [token][pairs], pairs = rot / 2 rounded up to whole chunks.  The places behind
 // rot / 2 are no pair's, but a lane with fewer than 8 pairs turns zeros by them, and those take part in the head's sums: they
 // get no rotation, as what LDS holds may be an infinity or NaN.
@@ -189,13 +196,26 @@ __global__ __launch_bounds__(QK_THREADS, BACKWARD ? 3 : 5) void qk_norm_rope_ker
 #pragma unroll
       for (int e = 0; e < 8; ++e) { a[e] = (float)w.va[e]; b[e] = (float)w.vb[e]; }
       if constexpr (!BACKWARD) {
-        float sq = 0.f;
+        auto mean_square = [&]() {
+          float sq = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sq += mine_a(e) ? a[e] * a[e] : 0.f;
-          sq += mine_b(e) ? b[e] * b[e] : 0.f;
+          for (int e = 0; e < 8; ++e) {
+            sq += mine_a(e) ? a[e] * a[e] : 0.f;
+            sq += mine_b(e) ? b[e] * b[e] : 0.f;
+          }
+          return head_sum<LPH>(sq) * inv_d;
+        };
+        float v = mean_square() + g.eps;
+        if (__any(qk_out_of_range(v))) {                // (heads of the wave that are in range come out as before)
+          const float s = qk_range_scale(v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            a[e] *= s;
+            b[e] *= s;
+          }
+          v = mean_square() + g.eps * s * s;
         }
-        const float r = rsqrtf(head_sum<LPH>(sq) * inv_d + g.eps);
+        const float r = rsqrtf(v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           a[e] *= r * gain[0][e];
@@ -204,22 +224,41 @@ __global__ __launch_bounds__(QK_THREADS, BACKWARD ? 3 : 5) void qk_norm_rope_ker
         if (l.pair_a >= 0) qk_turn<INTERLEAVED, false>(a, b, cs, l);
       } else {
         if (l.pair_a >= 0) qk_turn<INTERLEAVED, true>(a, b, cs, l);
-        float sq = 0.f, dot = 0.f;
+        float xa[8], xb[8], s = 1.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float xa = mine_a(e) ? (float)w.xa[e] : 0.f, xb = mine_b(e) ? (float)w.xb[e] : 0.f;
-          sq += xa * xa + xb * xb;
-          dot += a[e] * gain[0][e] * xa + b[e] * gain[1][e] * xb;
+        for (int e = 0; e < 8; ++e) { xa[e] = (float)w.xa[e]; xb[e] = (float)w.xb[e]; }
+        float sq, dot;
+        auto sums = [&]() {
+          sq = dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float ma = mine_a(e) ? xa[e] : 0.f, mb = mine_b(e) ? xb[e] : 0.f;
+            sq += ma * ma + mb * mb;
+            dot += a[e] * gain[0][e] * ma + b[e] * gain[1][e] * mb;
+          }
+          sq = head_sum<LPH>(sq) * inv_d;
+        };
+        sums();
+        float v = sq + g.eps;
+        if (__any(qk_out_of_range(v))) {
+          s = qk_range_scale(v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            xa[e] *= s;
+            xb[e] *= s;
+          }
+          sums();
+          v = sq + g.eps * s * s;
         }
-        const float r = rsqrtf(head_sum<LPH>(sq) * inv_d + g.eps);
+        const float r = rsqrtf(v), rs = r * s;          // of the multiplied head; of x
         const float m = head_sum<LPH>(dot) * r * inv_d;                  // mean(w xh)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float ha = r * (float)w.xa[e], hb = r * (float)w.xb[e];
+          const float ha = r * xa[e], hb = r * xb[e];
           sum[0][e] += a[e] * ha;                       // (of elements that are another lane's as well: not looked at)
           sum[1][e] += b[e] * hb;
-          a[e] = r * (a[e] * gain[0][e] - ha * m);
-          b[e] = r * (b[e] * gain[1][e] - hb * m);
+          a[e] = rs * (a[e] * gain[0][e] - ha * m);
+          b[e] = rs * (b[e] * gain[1][e] - hb * m);
         }
       }
       elemx8 oa, ob;
