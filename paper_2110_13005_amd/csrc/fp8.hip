@@ -858,34 +858,16 @@ static hipError_t launch_fp8_big(Fp8Args g, hipStream_t s) {
   hipLaunchKernelGGL(HIP_KERNEL_NAME(gemm_fp8_big_kernel<EPI>), dim3((unsigned)std::min(256, g.tiles_m * g.tiles_n)), dim3(256), 0, s, g);
   return hipGetLastError();
 }
-// The kernel with the least modelled time: rounds of workgroups, each a fixed part and a part per 128 of k, in us.  The parts are
-// from single launches of outputs of 200 x 392 to 8192 x 20480 with K = 512 to 16384; a CU that is shared is slower per step.
-// Modelled / measured, 64 x 64, 128 x 128 and 256 x 256: 512 x 512 x 4096 8.8 / 8.9, 14 / 13, 43 / 42;  2048^3 17 / 16,
-// 9.4 / 10.9, 27 / 27;  2047 x 2048 x 8192 57 / 57, 31 / 32, 80 / 78;  2048 x 6144 x 2048 (two thirds of the CUs for the
-// last) 51 / 44, 28 / 31, 29 / 31;  4096^3 122 / 101, 67 / 70, 52 / 55.
 template <int EPI>
 static hipError_t launch_fp8(const Fp8Args& g, hipStream_t s) {
-  auto tiles = [&](int64_t bm, int64_t bn) { return (g.M + bm - 1) / bm * ((g.N + bn - 1) / bn); };
-  const int64_t t64 = tiles(64, 64), t128 = tiles(128, 128), t256 = tiles(256, 256);
-  auto rounds = [](int64_t t, int64_t per) { return (double)((t + per - 1) / per); };
+  const int tile = host::choose_fp8_tile(g.M, g.N, g.nk, EPI == EPI_ACC_F32);
+  if (tile == host::FP8_64x64) return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
   if constexpr (EPI == EPI_ACC_F32) {
-    // bf16 MFMAs, with a part for the results' stores.  256 x 256 tiles by eight waves of 128 x 64 convert a code 1.5 times per
-    // matrix instruction, 128 x 128 by four of 64 x 64 twice.  Modelled / measured, 64 x 64, 128 x 128 and 256 x 256:
-    // 512 x 512 x 4096 14 / 15, 32 / 33, 77 / 82;  2048^3 24 / 25, 23 / 23, 45 / 47;  2048 x 8192 x 2047 94 / 91, 65 / 66, 56 / 59;
-    // 1536 x 6144 x 8192 212 / 172, 223 / 156, 166 / 160;  8192^3 on the last two 893 / 850, 722 / 733 (1500 TFLOP/s).
-    const double small = rounds(t64, 512) * (1.5 + g.nk * (t64 > 256 ? 0.64 : 0.39));
-    const double mid = rounds(t128, 512) * (2.5 + 3.5 * std::min(1.0, t128 / 512.0) + g.nk * (t128 > 256 ? 1.65 : t128 > 128 ? 1.2 : 0.91));
-    const double big = rounds(t256, 256) * (6.0 + 8.0 * std::min(1.0, t256 / 256.0) + g.nk * (2.2 + 0.4 * std::min(1.0, t256 / 256.0)));
-    if (big < mid && big < small) return launch_fp8_tile<2, 4, 8, 4, 2, EPI>(g, s);
-    if (mid < small) return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
-    return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
+    if (tile == host::FP8_256x256) return launch_fp8_tile<2, 4, 8, 4, 2, EPI>(g, s);
+    return launch_fp8_tile<2, 2, 4, 4, 2, EPI>(g, s);
   } else {
-    const double small = rounds(t64, 512) * (1.8 + g.nk * (t64 > 256 ? 0.42 : 0.22));
-    const double mid = rounds(t128, 256) * (2.0 + g.nk * (0.37 + 0.09 * std::min(1.0, t128 / 256.0)));
-    const double big = 4.0 + rounds(t256, 256) * (5.0 + (g.nk + 3) / 4 * 4 * (1.05 + 0.3 * std::min(1.0, t256 / 256.0)));
-    if (big < mid && big < small) return launch_fp8_big<EPI>(g, s);
-    if (mid < small) return launch_fp8_mid<EPI>(g, s);
-    return launch_fp8_tile<2, 2, 2, 2, 4, EPI>(g, s);
+    if (tile == host::FP8_256x256) return launch_fp8_big<EPI>(g, s);
+    return launch_fp8_mid<EPI>(g, s);
   }
 }
 

@@ -2,7 +2,7 @@
 // takes next, the bookkeeping of the activation stash slots (Sec. 3.3: at most pipeline_limit microbatches in
 // flight), when the deferred weight gradients of a group of microbatches are formed, how long the loop waits
 // for a message, and the bucket plan of the offloaded optimizer (Sec. 5.2) with the chunks of the step that
-// overlaps the backward tail (Sec. 5.3); and the tile a GEMM launch takes with the order of its workgroups (gemm.hip).
+// overlaps the backward tail (Sec. 5.3); and the tile a GEMM launch takes with the order of its workgroups (gemm.hip, fp8.hip).
 // stage.cpp calls these with its HIP streams and events around them; the CPU tests compile this header alone (with the
 // address, undefined-behaviour and thread sanitizers) and drive it with simulated events.
 #pragma once
@@ -474,6 +474,34 @@ inline RingSplit choose_split(int64_t M, int64_t N, int64_t K, int64_t forced) {
       if (cost < best_cost) { best = {t, parts}; best_cost = cost; }
     }
   return best;
+}
+
+// ------------------------------------------------------------------------------ tiles of the 8-bit product's launcher
+// Tile of the kernel with the least modelled time: rounds of workgroups, each a fixed part and a part per 128 of k (nk), in us.  The
+// parts are from single launches of outputs of 200 x 392 to 8192 x 20480 with K = 512 to 16384; a CU that is shared is slower per step.
+// Modelled / measured, 64 x 64, 128 x 128 and 256 x 256: 512 x 512 x 4096 8.8 / 8.9, 14 / 13, 43 / 42;  2048^3 17 / 16,
+// 9.4 / 10.9, 27 / 27;  2047 x 2048 x 8192 57 / 57, 31 / 32, 80 / 78;  2048 x 6144 x 2048 (two thirds of the CUs for the
+// last) 51 / 44, 28 / 31, 29 / 31;  4096^3 122 / 101, 67 / 70, 52 / 55.
+// 32-bit results (bf16 MFMAs) have kernels of their own, with a part for the stores.  256 x 256 tiles by eight waves of 128 x 64 convert
+// a code 1.5 times per matrix instruction, 128 x 128 by four of 64 x 64 twice.  Modelled / measured, 64 x 64, 128 x 128 and 256 x 256:
+// 512 x 512 x 4096 14 / 15, 32 / 33, 77 / 82;  2048^3 24 / 25, 23 / 23, 45 / 47;  2048 x 8192 x 2047 94 / 91, 65 / 66, 56 / 59;
+// 1536 x 6144 x 8192 212 / 172, 223 / 156, 166 / 160;  8192^3 on the last two 893 / 850, 722 / 733 (1500 TFLOP/s).
+enum Fp8Tile { FP8_64x64, FP8_128x128, FP8_256x256 };
+inline int choose_fp8_tile(int64_t M, int64_t N, int64_t nk, bool fp32_result) {
+  const auto tiles = [&](int64_t width) { return (M + width - 1) / width * ((N + width - 1) / width); };
+  const auto rounds = [](int64_t t, int64_t per) { return (double)((t + per - 1) / per); };
+  const int64_t t64 = tiles(64), t128 = tiles(128), t256 = tiles(256);
+  double small, mid, big;
+  if (fp32_result) {
+    small = rounds(t64, 512) * (1.5 + nk * (t64 > 256 ? 0.64 : 0.39));
+    mid = rounds(t128, 512) * (2.5 + 3.5 * std::min(1.0, t128 / 512.0) + nk * (t128 > 256 ? 1.65 : t128 > 128 ? 1.2 : 0.91));
+    big = rounds(t256, 256) * (6.0 + 8.0 * std::min(1.0, t256 / 256.0) + nk * (2.2 + 0.4 * std::min(1.0, t256 / 256.0)));
+  } else {
+    small = rounds(t64, 512) * (1.8 + nk * (t64 > 256 ? 0.42 : 0.22));
+    mid = rounds(t128, 256) * (2.0 + nk * (0.37 + 0.09 * std::min(1.0, t128 / 256.0)));
+    big = 4.0 + rounds(t256, 256) * (5.0 + (nk + 3) / 4 * 4 * (1.05 + 0.3 * std::min(1.0, t256 / 256.0)));
+  }
+  return big < mid && big < small ? FP8_256x256 : mid < small ? FP8_128x128 : FP8_64x64;
 }
 
 }  // namespace host
