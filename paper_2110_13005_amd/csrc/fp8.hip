@@ -254,9 +254,13 @@ hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x
 // The B fragment goes first: lane l then holds row l % 16 of C and columns 4 * (l / 16) + 0..3.
 //
 // How exact it is: within groups of 8 k the matrix unit drops what lies more than 13 binary places below the group's largest
-// product (measured: 2^16 + 2^2 gives 2^16; the groups, and the instructions, are added in fp32), about 1.5e-5 of a result.
-// A 16-bit result does not show it (2e-3 or 2.4e-4 of rounding); 32-bit results (EPI_ACC_F32) are therefore formed
-// with the bf16 MFMA, whose sums are exact to fp32, from codes converted in registers with their scale.
+// product (measured: 2^16 + 2^2 gives 2^16, 2^16 + 2^3 is exact; the groups, and the instructions, are added in fp32).  Each of seven
+// products loses less than 2^-13 of the largest, so a sum is off by at most 7 * 2^-13 of its products' magnitudes: on random data 1.5e-5
+// of a result, but with cancellation any part of it.  16-bit results are formed this way by choice: on random data the distance from the
+// exact result stays that of the rounding (bf16 1.66e-3 of the result in the root mean square with either kind of sum, fp16 2.08e-4; 1 %
+// and 6 % of the elements differ, by one step), a code itself is off by up to 2^-4 of its number, and the exact way is half as fast
+// (8192^3 733 us, this way 381).  Who needs the sums themselves takes 32-bit results (EPI_ACC_F32): those are formed with the bf16 MFMA,
+// whose sums are exact to fp32, from codes converted in registers with their scale.
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
