@@ -507,7 +507,8 @@ int axonn_embedding_bwd(int64_t T, int64_t h, int64_t vocab, const int32_t* toke
  * interleaved; elements from rotary_dim on are not rotated.  The position of token t is
  * positions[t] (device, any int32), or t % seq_len if positions is NULL.  inv_freq: device array
  * of rotary_dim / 2 doubles (e.g. base^(-2i / rotary_dim); NULL allowed if rotary_dim is 0).
- * head_dim even, at most 256; rotary_dim even, at most head_dim; eps > 0; T <= 2^24.
+ * head_dim even, at most 256; rotary_dim even, at most head_dim; n_heads, n_kv_heads <= 4096;
+ * eps > 0; T <= 2^24.
  * out may be qkv (V is then left alone); columns of out behind the three parts are not written. */
 int axonn_qk_norm_rope_fwd(int64_t T, int32_t seq_len, int32_t n_heads, int32_t n_kv_heads,
                            int32_t head_dim, int32_t rotary_dim, int32_t interleaved,
@@ -539,7 +540,8 @@ int axonn_qk_norm_rope_bwd(int64_t T, int32_t seq_len, int32_t n_heads, int32_t 
  * halves, low first, of the four words for key (seed low, seed high) and counter (g, r, offset
  * low, offset high); an element is kept if its half is >= round(65536 p).
  * offset_dev: NULL, or one device uint64 that is added to offset when the kernel runs (a captured
- * graph reads it anew at every replay).  out may be x or res.  T, h <= 2^24. */
+ * graph reads it anew at every replay).  out may be x or res.  T, h <= 2^24,
+ * T * ceil(h / 8) <= 2^33. */
 int axonn_dropout_fwd(int64_t T, int64_t h, const void* x_bf16, int64_t ld_x,
                       const void* res_bf16, int64_t ld_res, float p, uint64_t seed,
                       uint64_t offset, const uint64_t* offset_dev, void* out_bf16,

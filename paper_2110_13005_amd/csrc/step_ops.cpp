@@ -52,7 +52,7 @@ int dropout(const char* what, int64_t T, int64_t h, const void* x, int64_t ld_x,
   if (T < 1 || h < 1) return fail_entry(AXONN_EINVAL, "%s: non-positive size", what);
   if (!(p >= 0.f && p <= 1.f)) return fail_entry(AXONN_EINVAL, "%s: p must be in [0, 1]", what);
   if (T > kMaxRows || h > kMaxRows || T * ((h + 7) / 8) > (int64_t(1) << 33))
-    return fail_entry(AXONN_EUNSUPPORTED, "%s: at most 2^24 rows, 2^24 columns and 2^36 elements", what);
+    return fail_entry(AXONN_EUNSUPPORTED, "%s: at most 2^24 rows, 2^24 columns and 2^33 groups of 8 columns over all rows", what);
   if (ld_x < h || ld_out < h || (res && ld_res < h)) return fail_entry(AXONN_EINVAL, "%s: leading dimension too small", what);
   if ((out == x && ld_out != ld_x) || (out == res && ld_out != ld_res))
     return fail_entry(AXONN_EINVAL, "%s: in place with two leading dimensions", what);
