@@ -6,7 +6,8 @@
 // (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011), and an element is kept if its half is at
 // least thr = round(65536 p).  Kept elements are multiplied by 65536 / (65536 - thr), the reciprocal of the probability with
 // which they are kept, so the rounding of p leaves the expectation as it is.  32 bits per element would be twice the generator's
-// work, which then bounds the kernel; this way HBM does: 16384 x 5120 with a residual in 89 us (5.7 TB/s), 4096 x 4512 without in 15.
+// work, which then bounds the kernel; this way HBM does: 16384 x 5120 with a residual in 89 to 93 us (5.4 to 5.7 TB/s), 4096 x 4512
+// without in 15.
 #include "rows.h"
 #include "host_logic.h"
 #include <type_traits>
@@ -92,8 +93,8 @@ hipError_t launch_dropout(int64_t T, int64_t h, const void* x, int64_t ld_x, con
   g.key0 = (uint32_t)seed; g.key1 = (uint32_t)(seed >> 32);
   g.scale = threshold < 65536u ? (float)(65536.0 / (65536.0 - threshold)) : 0.f;
   g.offset = offset; g.offset_dev = offset_dev;
-  // four chunks per lane (their loads in flight together) where that leaves every CU two workgroups; else one: 7 x 1001 takes 2.7 us,
-  // with four 5.6
+  // four chunks per lane (their loads in flight together) where that leaves every CU two workgroups; else one: 7 x 1001 takes 2.9 us
+  // in the kernel trace, with four 6.3
   const auto launch = [&](auto chunks) {
     constexpr int CHUNKS = decltype(chunks)::value;
     const dim3 blocks((unsigned)((g.n_chunks + DO_THREADS * CHUNKS - 1) / (DO_THREADS * CHUNKS)));

@@ -259,7 +259,7 @@ hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x
 // of a result, but with cancellation any part of it.  16-bit results are formed this way by choice: on random data the distance from the
 // exact result stays that of the rounding (bf16 1.66e-3 of the result in the root mean square with either kind of sum, fp16 2.08e-4; 1 %
 // and 6 % of the elements differ, by one step), a code itself is off by up to 2^-4 of its number, and the exact way is half as fast
-// (8192^3 733 us, this way 381).  Who needs the sums themselves takes 32-bit results (EPI_ACC_F32): those are formed with the bf16 MFMA,
+// (8192^3 733 to 756 us, this way 382).  Who needs the sums themselves takes 32-bit results (EPI_ACC_F32): those are formed with the bf16 MFMA,
 // whose sums are exact to fp32, from codes converted in registers with their scale.
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -629,9 +629,10 @@ __global__ __launch_bounds__(256) void gemm_fp8_mid_kernel(const Fp8Args g) {
 
 // The product for problems that fill the chip with 256 x 256 tiles: four waves, one per SIMD, each 128 x 128 of the result, the
 // 256 accumulators in the accumulation registers.  With 8 waves of 128 x 64 (196 KB of fragments per tile of k instead of 128 KB,
-// and every wave at the barrier with nothing to do) the product of 8192 x 5120 x 20480 took 1000 us, this way 725 (2370 TFLOP/s;
-// 8192^3 381 us, 2880).  The matrix units are busy 77 % of the cycles there, at the 1.75 GHz that the chip's power leaves (zeros for
-// operands: 3200).
+// and every wave at the barrier with nothing to do) 8192 x 20480 results over K = 5120 took 1.35 times as long (1000 us and 745, single
+// launches behind pauses).  Launches one behind the other, 24 at a time, take 633 us (2710 TFLOP/s), 8192^3 382 (2880); a few behind a
+// pause 654 to 791, and so under the profiler, 736.  The matrix units are busy 77 % of the cycles of 8192^3, at the 1.75 GHz that the
+// chip's power leaves (zeros for operands: 3200).
 //
 // Half a tile of k (the rows of four of the eight fragments) is the unit of copying: a set holds half of A(kt) and half of
 // B(kt + 1), 16 KB each, four sets in LDS.  A group is the 8 MFMAs of one A fragment; while it runs, the next A fragment and one B

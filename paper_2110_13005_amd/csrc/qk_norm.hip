@@ -7,7 +7,7 @@
 // The angle of pair i is position * inv_freq[i], formed in 64 bits and reduced to a fraction of a turn there, so that far
 // positions keep their place on the circle; sine and cosine are computed once per token and pair and shared by the heads
 // through LDS.  Sums and the arithmetic are fp32, with one rounding at the end.  HBM-bound: each row is read and written once;
-// 8192 tokens x 40 query and 40 key heads of 128 forward in 96 to 105 us (503 MB, 4.8 to 5.2 TB/s), 4096 x (32, 8) backward in 29 us
+// 8192 tokens x 40 query and 40 key heads of 128 forward in 96 to 105 us (503 MB, 4.8 to 5.2 TB/s), 4096 x (32, 8) backward in 29 to 32 us
 // (143 MB, 4.9) and 4 for the gains' sums.
 //
 // A head belongs to LPH lanes; a lane holds 8 pairs, a[8] and b[8]: of the rotated part, a chunk of the first half and the
