@@ -46,3 +46,9 @@ def test_one_block_never_takes_the_largest_tiles(tmp_path):
 def test_the_launcher_takes_the_function_that_is_tested():
     src = open(os.path.join(os.path.dirname(HERE), "paper_2110_13005_amd", "csrc", "fp8.hip")).read()
     assert "host::choose_fp8_tile" in src
+
+
+def test_the_product_that_leaves_nan_in_lds(tmp_path):
+    """test_gpu_qk_norm_values.py fills the LDS with the kernel of 128 x 128 tiles, which copies whole tiles to its end (that of 256 x 256
+    clears most of it)."""
+    assert choices(tmp_path, [(2048, 2048, 512, 0)]) == [128]
