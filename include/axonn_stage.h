@@ -582,6 +582,106 @@ int axonn_gemm_fp8(int32_t epilogue, int64_t M, int64_t N, int64_t K, const void
                    int64_t ld_aux, int32_t accumulate, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------
+ * Training steps on packed sequences: n_seq sequences of different lengths lie one behind the other
+ * in T rows (tokens), sequence i in rows offsets[i] .. offsets[i + 1] - 1 (offsets: device int32
+ * [n_seq + 1], ascending, 0 .. T; a sequence may be empty).  Attention inside the sequences, and
+ * losses over their logits: a clipped policy loss, a preference loss of pairs, distillation from a
+ * teacher's top logits.  The conventions of the operations of a training step above hold.
+ * ---------------------------------------------------------------------------------- */
+
+/* The tiles that attention takes the sequences in, those with the most work first.  A plan serves all
+ * calls, forward and backward, with these offsets and this T and n_seq (any heads, any layer); a
+ * captured graph that holds this call forms it anew at every replay.  Offsets are read when the work
+ * runs; one that is smaller than one in front of it is taken as that one, and all are clamped to
+ * [0, T].  plan: the number of bytes that _plan_bytes returns, 16-byte aligned; it has to have been
+ * formed in front of the calls that read it.  T <= 2^24, n_seq <= 2^20. */
+int axonn_attention_packed_plan_bytes(int64_t T, int32_t n_seq, uint64_t* bytes);
+int axonn_attention_packed_plan(int64_t T, int32_t n_seq, const int32_t* offsets, void* plan,
+                                void* hip_stream);
+/* Causal self-attention inside each sequence over packed rows [Q | K | V] of n_heads, n_kv_heads and
+ * n_kv_heads heads (the layout of axonn_qk_norm_rope_fwd); query head j reads key / value head
+ * j / (n_heads / n_kv_heads).  With i, j positions in a sequence:
+ *   o_i = sum_j<=i P_ij v_j,   P_ij = exp(scale q_i.k_j - lse_i),   lse_i = log sum_j<=i exp(scale q_i.k_j)
+ * o [T, n_heads * head_dim]; lse [n_heads][T] float32.  Rows of o and lse that belong to no sequence are
+ * left as they are, and nothing that lies in another row than a sequence's reaches its results.
+ * head_dim a multiple of 4, at most 192; n_heads a multiple of n_kv_heads, at most 4096;
+ * T * n_heads <= 2^27, n_seq * n_heads <= 2^23; leading dimensions at most 2^22; scale > 0
+ * (usually 1 / sqrt(head_dim)). */
+int axonn_attention_packed_fwd(int64_t T, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
+                               int32_t head_dim, float scale, const void* plan,
+                               const void* qkv_bf16, int64_t ld_qkv, void* o_bf16, int64_t ld_o,
+                               float* lse, void* hip_stream);
+/* Its gradient: dqkv (rows like qkv's) from dout, o and lse; the gradients of a key / value head are
+ * the sums over the query heads that read it.  Rows of dqkv that belong to no sequence are left as
+ * they are; the result has the same bits every time.  workspace: the number of bytes that _workspace
+ * returns, 16-byte aligned. */
+int axonn_attention_packed_bwd_workspace(int64_t T, int32_t n_seq, int32_t n_heads,
+                                         int32_t n_kv_heads, int32_t head_dim, uint64_t* bytes);
+int axonn_attention_packed_bwd(int64_t T, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
+                               int32_t head_dim, float scale, const void* plan,
+                               const void* qkv_bf16, int64_t ld_qkv, const void* o_bf16,
+                               int64_t ld_o, const float* lse, const void* dout_bf16,
+                               int64_t ld_dout, void* dqkv_bf16, int64_t ld_dqkv, void* workspace,
+                               void* hip_stream);
+
+/* Of logits [T, V]: logp[t] = z[target] - lse, lse[t] = log sum_v exp(z[v]), both float32.  A token
+ * whose target is outside [0, V) has no part: its row is not read, logp and lse are 0.
+ * T <= 2^22, V <= 2^20, here and in the losses below. */
+int axonn_token_logprobs_fwd(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_logits,
+                             const int32_t* targets, float* logp, float* lse, void* hip_stream);
+/* Its gradient: dlogits = dlogp[t] (onehot(target) - softmax(z)); rows of zeros for tokens without a
+ * target and where dlogp[t] is 0.  dlogits may be logits. */
+int axonn_token_logprobs_bwd(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_logits,
+                             const int32_t* targets, const float* lse, const float* dlogp,
+                             void* dlogits_bf16, int64_t ld_dlogits, void* hip_stream);
+
+/* Clipped policy loss with a KL term, and its gradient, from logits [T, V].  With the ratio
+ * r = exp(logp - old_logp[t]), A = advantage[t] and x = ref_logp[t] - logp:
+ *   token_loss[t] = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(x) - x - 1)
+ *   loss[0] = sum_t weight[t] token_loss[t]
+ *   dlogits = loss_scale d loss / d logits       (a clipped token has the KL term's gradient alone)
+ * Tokens whose target is outside [0, V) or whose weight is 0 have no part: their logits are not read,
+ * logp and token_loss are 0, their rows of dlogits zeros.  ref_logp may be NULL if kl_coef is 0; logp
+ * and loss may be NULL; so may dlogits (losses alone), or it may be logits.  clip_low in [0, 1]. */
+int axonn_policy_loss(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_logits,
+                      const int32_t* targets, const float* old_logp, const float* ref_logp,
+                      const float* advantage, const float* weight, float clip_low, float clip_high,
+                      float kl_coef, float loss_scale, float* logp, float* token_loss, float* loss,
+                      void* dlogits_bf16, int64_t ld_dlogits, void* hip_stream);
+
+/* Preference loss of n_pairs pairs of sequences from their tokens' log-probabilities: of the 2 n_pairs
+ * sequences (offsets: [2 n_pairs + 1]) 2i is the chosen and 2i + 1 the rejected answer of pair i.  With
+ * the margin m = beta (sum over the chosen - sum over the rejected tokens of (logp - ref_logp)):
+ *   pair_loss[i] = -(1 - label_smoothing) log sigma(m) - label_smoothing log sigma(-m)
+ *   loss[0] = scale sum_i pair_loss[i],   dlogp[t] = loss_scale d loss / d logp[t]
+ * Tokens whose target is outside [0, V) have no part, like those that belong to no sequence: dlogp is 0
+ * there.  The sums over tokens are formed in 64 bits.  ref_logp (NULL: zeros) and loss may be NULL.
+ * axonn_token_logprobs_fwd in front and _bwd behind make it a loss over logits. */
+int axonn_preference_loss(int64_t T, int32_t n_pairs, int64_t V, const int32_t* offsets,
+                          const int32_t* targets, const float* logp, const float* ref_logp,
+                          float beta, float label_smoothing, float scale, float loss_scale,
+                          float* pair_loss, float* loss, float* dlogp, void* hip_stream);
+
+/* Distillation from a teacher's top logits, and its gradient.  Of every token t the teacher has named up
+ * to K tokens teacher_ids[t][0..K) (int32; one outside [0, V) stands for none) with logits
+ * teacher_logits[t][0..K) (float32); both have rows of ld_teacher.  With the student's
+ * q = softmax(z / temperature):
+ *   teacher_lse NULL:  p = softmax(teacher_logits / temperature) over the named tokens,
+ *                      token_loss = sum_j p_j (log p_j - log q_j)
+ *   else               p_j = exp(teacher_logits_j / temperature - teacher_lse[t]), and the mass of all other
+ *                      tokens is one more outcome: + P (log P - log Q), P = max(1 - sum_j p_j, 0),
+ *                      Q = the student's mass of the tokens that are not named
+ *   loss[0] = sum_t weight[t] token_loss[t],   dlogits = loss_scale d loss / d logits
+ * A token named twice counts as two entries.  Rows in which no token is named, or whose weight is 0, have
+ * no part: token_loss 0, dlogits zeros (the logits are not read).  loss may be NULL; so may dlogits, or it
+ * may be logits.  K <= 1024, V <= 393216. */
+int axonn_distill_loss(int64_t T, int64_t V, int32_t K, const void* logits_bf16, int64_t ld_logits,
+                       const float* teacher_logits, const int32_t* teacher_ids, int64_t ld_teacher,
+                       const float* teacher_lse, float temperature, const float* weight,
+                       float loss_scale, float* token_loss, float* loss, void* dlogits_bf16,
+                       int64_t ld_dlogits, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------
  * Launch timing (measurement aid, off by default).  While enabled, every kernel launch the
  * library makes is bracketed by a pair of HIP events on the stream it is launched on;
  * collect() waits for them, adds up elapsed milliseconds and launch counts per category
@@ -590,7 +690,7 @@ int axonn_gemm_fp8(int32_t epilogue, int64_t M, int64_t N, int64_t K, const void
  * forms several weight gradients counts as that many), attention
  * forward / backward, LayerNorm forward / backward (the backward with the reduction of its
  * gain and shift gradients), gradient conversion, Adam, input copy, embedding,
- * cross-entropy, query / key norms with rotation, dropout, 8-bit quantiser, 8-bit products.  Process-wide, not thread-safe.  Intervals of kernels that overlap on different streams are each counted
+ * cross-entropy, query / key norms with rotation, dropout, 8-bit quantiser, 8-bit products, losses over logits.  Process-wide, not thread-safe.  Intervals of kernels that overlap on different streams are each counted
  * in full.
  * ---------------------------------------------------------------------------------- */
 int axonn_profile_enable(int32_t on);

@@ -134,6 +134,16 @@ _PROTOTYPES = {
     "axonn_dropout_bwd": [_i64, _i64, _vp, _i64, _f, _u64, _u64, _vp, _vp, _i64, _vp],
     "axonn_fp8_quantize": [_i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp],
     "axonn_gemm_fp8": [_i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _i32, _vp],
+    "axonn_attention_packed_plan_bytes": [_i64, _i32, C.POINTER(_u64)],
+    "axonn_attention_packed_plan": [_i64, _i32, _vp, _vp, _vp],
+    "axonn_attention_packed_fwd": [_i64, _i32, _i32, _i32, _i32, _f, _vp, _vp, _i64, _vp, _i64, _vp, _vp],
+    "axonn_attention_packed_bwd_workspace": [_i64, _i32, _i32, _i32, _i32, C.POINTER(_u64)],
+    "axonn_attention_packed_bwd": [_i64, _i32, _i32, _i32, _i32, _f, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _vp],
+    "axonn_token_logprobs_fwd": [_i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp],
+    "axonn_token_logprobs_bwd": [_i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _i64, _vp],
+    "axonn_policy_loss": [_i64, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _f, _f, _f, _f, _vp, _vp, _vp, _vp, _i64, _vp],
+    "axonn_preference_loss": [_i64, _i32, _i64, _vp, _vp, _vp, _vp, _f, _f, _f, _f, _vp, _vp, _vp, _vp],
+    "axonn_distill_loss": [_i64, _i64, _i32, _vp, _i64, _vp, _vp, _i64, _vp, _f, _vp, _f, _vp, _vp, _vp, _i64, _vp],
     "axonn_profile_enable": [_i32],
     "axonn_profile_num_categories": [C.POINTER(_i32)],
     "axonn_profile_category_name": [_i32, C.POINTER(C.c_char_p)],
@@ -565,6 +575,62 @@ def axonn_gemm_fp8(epilogue, M, N, K, A, a_scale, B, b_scale, Cmat, ldc, bias=No
                    accumulate=0, stream=None):
     _call("axonn_gemm_fp8", epilogue, M, N, K, _ptr(A), _ptr(a_scale), _ptr(B), _ptr(b_scale), _ptr(Cmat), ldc, _ptr(bias), _ptr(res),
           ld_res, _ptr(aux), ld_aux, accumulate, _stream(stream))
+
+
+def axonn_attention_packed_plan_bytes(T, n_seq):
+    """Bytes of the plan of n_seq sequences in T rows."""
+    n = _u64()
+    _call("axonn_attention_packed_plan_bytes", T, n_seq, C.byref(n))
+    return n.value
+
+
+def axonn_attention_packed_plan(T, n_seq, offsets, plan, stream=None):
+    _call("axonn_attention_packed_plan", T, n_seq, _ptr(offsets), _ptr(plan), _stream(stream))
+
+
+def axonn_attention_packed_fwd(T, n_seq, n_heads, n_kv_heads, head_dim, scale, plan, qkv, ld_qkv, o, ld_o, lse, stream=None):
+    _call("axonn_attention_packed_fwd", T, n_seq, n_heads, n_kv_heads, head_dim, scale, _ptr(plan), _ptr(qkv), ld_qkv, _ptr(o), ld_o,
+          _ptr(lse), _stream(stream))
+
+
+def axonn_attention_packed_bwd_workspace(T, n_seq, n_heads, n_kv_heads, head_dim):
+    """Bytes of workspace that axonn_attention_packed_bwd needs."""
+    n = _u64()
+    _call("axonn_attention_packed_bwd_workspace", T, n_seq, n_heads, n_kv_heads, head_dim, C.byref(n))
+    return n.value
+
+
+def axonn_attention_packed_bwd(T, n_seq, n_heads, n_kv_heads, head_dim, scale, plan, qkv, ld_qkv, o, ld_o, lse, dout, ld_dout, dqkv,
+                               ld_dqkv, workspace, stream=None):
+    _call("axonn_attention_packed_bwd", T, n_seq, n_heads, n_kv_heads, head_dim, scale, _ptr(plan), _ptr(qkv), ld_qkv, _ptr(o), ld_o,
+          _ptr(lse), _ptr(dout), ld_dout, _ptr(dqkv), ld_dqkv, _ptr(workspace), _stream(stream))
+
+
+def axonn_token_logprobs_fwd(T, V, logits, ld_logits, targets, logp, lse, stream=None):
+    _call("axonn_token_logprobs_fwd", T, V, _ptr(logits), ld_logits, _ptr(targets), _ptr(logp), _ptr(lse), _stream(stream))
+
+
+def axonn_token_logprobs_bwd(T, V, logits, ld_logits, targets, lse, dlogp, dlogits, ld_dlogits, stream=None):
+    _call("axonn_token_logprobs_bwd", T, V, _ptr(logits), ld_logits, _ptr(targets), _ptr(lse), _ptr(dlogp), _ptr(dlogits), ld_dlogits,
+          _stream(stream))
+
+
+def axonn_policy_loss(T, V, logits, ld_logits, targets, old_logp, ref_logp, advantage, weight, clip_low, clip_high, kl_coef, loss_scale,
+                      logp, token_loss, loss, dlogits, ld_dlogits, stream=None):
+    _call("axonn_policy_loss", T, V, _ptr(logits), ld_logits, _ptr(targets), _ptr(old_logp), _ptr(ref_logp), _ptr(advantage), _ptr(weight),
+          clip_low, clip_high, kl_coef, loss_scale, _ptr(logp), _ptr(token_loss), _ptr(loss), _ptr(dlogits), ld_dlogits, _stream(stream))
+
+
+def axonn_preference_loss(T, n_pairs, V, offsets, targets, logp, ref_logp, beta, label_smoothing, scale, loss_scale, pair_loss, loss, dlogp,
+                          stream=None):
+    _call("axonn_preference_loss", T, n_pairs, V, _ptr(offsets), _ptr(targets), _ptr(logp), _ptr(ref_logp), beta, label_smoothing, scale,
+          loss_scale, _ptr(pair_loss), _ptr(loss), _ptr(dlogp), _stream(stream))
+
+
+def axonn_distill_loss(T, V, K, logits, ld_logits, teacher_logits, teacher_ids, ld_teacher, teacher_lse, temperature, weight, loss_scale,
+                       token_loss, loss, dlogits, ld_dlogits, stream=None):
+    _call("axonn_distill_loss", T, V, K, _ptr(logits), ld_logits, _ptr(teacher_logits), _ptr(teacher_ids), ld_teacher, _ptr(teacher_lse),
+          temperature, _ptr(weight), loss_scale, _ptr(token_loss), _ptr(loss), _ptr(dlogits), ld_dlogits, _stream(stream))
 
 
 TUNE_GEMM_COPY_MASK, TUNE_GEMM_BIG_MIN_TILES, TUNE_GEMM_TILE_N = 0, 1, 2

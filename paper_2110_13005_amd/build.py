@@ -14,8 +14,8 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libaxonn_stage.so")
 LIB_PATH_FP16 = os.path.join(HERE, "libaxonn_stage_fp16.so")
 VARIANTS = {"bf16": (LIB_PATH, []), "fp16": (LIB_PATH_FP16, ["-DAXONN_ELEM_FP16"])}
-SOURCES = ["gemm.hip", "attention.hip", "fp8.hip", "elementwise.hip", "lm_ends.hip", "stage.cpp", "qk_norm.hip", "embedding.hip",
-           "dropout.hip", "step_ops.cpp"]
+SOURCES = ["gemm.hip", "attention.hip", "attention_packed.hip", "fp8.hip", "elementwise.hip", "lm_ends.hip", "stage.cpp", "qk_norm.hip",
+           "embedding.hip", "losses.hip", "dropout.hip", "step_ops.cpp", "packed_ops.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

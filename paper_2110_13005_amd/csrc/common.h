@@ -365,6 +365,51 @@ hipError_t launch_fp8_quantize(int64_t R, int64_t C, const void* x, int64_t ld_x
 hipError_t launch_gemm_fp8(int epi, int64_t M, int64_t N, int64_t K, const void* A, const void* a_scale, const void* B, const void* b_scale,
                            void* C, int64_t ldc, const void* bias, const void* res, int64_t ld_res, void* aux, int64_t ld_aux,
                            int accumulate, hipStream_t s);
+// Operators on packed sequences (attention_packed.hip): n_seq sequences in T rows.
+struct PackedShape { int64_t T, n_seq; int heads, kv, d; float scale; };
+int64_t packed_tiles_bound(int64_t T, int64_t n_seq);
+uint64_t attention_packed_plan_size(int64_t T, int64_t n_seq);
+hipError_t launch_attention_packed_plan(int64_t T, int64_t n_seq, const int* offsets, void* plan, hipStream_t s);
+hipError_t launch_attention_packed_fwd(const PackedShape& p, const void* plan, const void* qkv, int64_t ld, void* o, int64_t ld_o, float* lse,
+                                       hipStream_t s);
+uint64_t attention_packed_bwd_ws_bytes(const PackedShape& p);
+hipError_t launch_attention_packed_bwd(const PackedShape& p, const void* plan, const void* qkv, int64_t ld, const void* o, int64_t ld_o,
+                                       const float* lse, const void* dout, int64_t ld_do, void* dqkv, int64_t ld_dqkv, void* workspace,
+                                       hipStream_t s);
+// Losses over logits [T, V] (losses.hip).  loss (may be null): one float, the weighted sum of the tokens' or pairs'.
+hipError_t launch_token_logprobs_fwd(int64_t T, int64_t V, const void* logits, int64_t ld, const int* targets, float* logp, float* lse,
+                                     hipStream_t s);
+hipError_t launch_token_logprobs_bwd(int64_t T, int64_t V, const void* logits, int64_t ld, const int* targets, const float* lse,
+                                     const float* dlogp, void* dlogits, int64_t ld_d, hipStream_t s);
+struct PolicyArgs {
+  int V;
+  const void* logits; int64_t ld;
+  const int* targets;
+  const float *old_logp, *ref_logp, *advantage, *weight;      // ref_logp may be null
+  float clip_low, clip_high, kl_coef, loss_scale;             // the ratio's limits
+  float *logp, *token_loss;                                   // logp may be null
+  void* dlogits; int64_t ld_d;                                // may be null
+};
+hipError_t launch_policy_loss(int64_t T, const PolicyArgs& p, float* loss, hipStream_t s);
+struct PreferenceArgs {
+  int T, n_pairs, V;
+  const int *offsets, *targets;
+  const float *logp, *ref_logp;                               // ref_logp may be null
+  float beta, smoothing, scale, loss_scale;
+  float *pair_loss, *dlogp;
+};
+hipError_t launch_preference_loss(const PreferenceArgs& p, float* loss, hipStream_t s);
+constexpr int kDistillMax = 1024, kDistillMaxVocab = 3 << 17;  // teacher's entries per token; their tokens' bits fit LDS
+struct DistillArgs {
+  int V, K;
+  const void* logits; int64_t ld;
+  const float* teacher; const int* ids; int64_t ld_teacher;
+  const float *teacher_lse, *weight;                          // teacher_lse may be null
+  float temperature, log2e_by_temperature, loss_scale;
+  float* token_loss;
+  void* dlogits; int64_t ld_d;                                // may be null
+};
+hipError_t launch_distill_loss(int64_t T, const DistillArgs& p, float* loss, hipStream_t s);
 hipError_t launch_adam(uint64_t n, float* theta, float* m, float* v, const void* g16,
                        void* p16, double lr, double b1, double b2, double eps, double wd,
                        int64_t step, double grad_scale, hipStream_t s);

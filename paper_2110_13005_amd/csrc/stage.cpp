@@ -45,18 +45,12 @@ int fail(int code, const char* fmt, ...) {
                   #expr, hipGetErrorString(e_));                                          \
   } while (0)
 
-#define AX_TRY(expr)       \
-  do {                     \
-    int r_ = (expr);       \
-    if (r_ != AXONN_OK) return r_; \
-  } while (0)
-
 
 // ---- optional per-launch timing: event pairs around every kernel launch, by category ----
 const char* const kProfNames[PC_COUNT] = {
     "gemm_fwd", "gemm_dgrad", "gemm_wgrad", "attention_fwd", "attention_bwd", "layernorm_fwd",
     "layernorm_bwd", "grad_convert", "adam", "copy_in", "embedding", "cross_entropy", "qk_norm_rope", "dropout",
-    "fp8_quantize", "gemm_fp8"};
+    "fp8_quantize", "gemm_fp8", "losses"};
 struct ProfRec { int cat, n; hipEvent_t a, b; };   // n: contractions of a launch that forms several
 bool g_prof_on = false;
 std::vector<ProfRec> g_prof_recs;

@@ -1,8 +1,6 @@
 // C entry points of the operations of a training step around the layer's own: scaled embedding, query / key norms with rotation,
 // dropout, 8-bit linear maps.  They check their arguments and launch (embedding.hip, qk_norm.hip, dropout.hip, fp8.hip); nothing is
 // allocated, nothing is kept between calls.
-#include "../../include/axonn_stage.h"
-#include "common.h"
 #include "entry.h"
 
 #include <cmath>
@@ -10,17 +8,6 @@
 using namespace axonn;
 
 namespace {
-
-#define AX_TRY(expr)       \
-  do {                     \
-    int r_ = (expr);       \
-    if (r_ != AXONN_OK) return r_; \
-  } while (0)
-
-int launched(hipError_t e, const char* what) {
-  if (e == hipSuccess) return AXONN_OK;
-  return fail_entry(AXONN_EHIP, "%s: kernel launch failed: %s", what, hipGetErrorString(e));
-}
 
 // Rows that a launch's grid can hold (its threads in one dimension are counted in 32 bits).
 constexpr int64_t kMaxRows = 1 << 24;

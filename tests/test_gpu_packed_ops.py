@@ -1,0 +1,274 @@
+"""GPU parity of attention over packed sequences with its float64 definition, element by element, at the lengths, head layouts, strides and
+values where it can go wrong; the plan that it follows; and a training step of packed operations as they are used together.
+
+Bounds: every rounding to 16 bits is off by half a step at most, fp32 arithmetic by U = 2^-24 of the magnitudes that go into it, counted
+along the formula (`attention_bounds`); a result is within what these add up to at worst."""
+import numpy as np
+import pytest
+
+from oracle import packed_ops as P
+from paper_2110_13005_amd import binding as B
+from helpers import dev_i32, host
+from test_gpu_step_ops import Padded, U, half_step, normal, within, workspace
+
+pytestmark = [pytest.mark.gpu, pytest.mark.parametrize("axonn_elem", ["bf16", "fp16"], indirect=True)]
+
+
+def surrounded(rows, cols, ld, shift, values, inside):
+    """A matrix among NaN: around it, and in its rows that belong to no sequence."""
+    import torch
+    m = Padded(rows, cols, ld, shift)
+    m.buf.fill_(float("nan"))
+    m.t[torch.from_numpy(inside).cuda()] = torch.from_numpy(np.ascontiguousarray(values[inside], np.float32)).cuda().to(m.buf.dtype)
+    return m
+
+
+def attention_bounds(qkv, dout, offsets, heads, kv, d, scale):
+    """-> how far o, lse and dqkv may be from their definitions (`within` adds the last rounding of the 16-bit ones)."""
+    h, T = half_step(), len(qkv)
+    tiny = 2.0 ** -25 if B.ELEM == "fp16" else 0.0                # half a step below half precision's smallest normal number
+    q, k, v = P._split(np.asarray(qkv, np.float64), heads, kv, d)
+    do = np.asarray(dout, np.float64).reshape(T, heads, d)
+    E_o, E_lse, E_g = np.zeros((T, heads, d)), np.zeros((heads, T)), np.zeros((T, heads + 2 * kv, d))
+    for a, b in P.sequences(offsets, T):
+        n = b - a
+        for i in range(heads if n else 0):
+            j = i // (heads // kv)
+            Q, K, V, D = q[a:b, i], k[a:b, j], v[a:b, j], do[a:b, i]
+            p, lse = P.attention_probabilities(Q, K, scale)
+            keep = np.tril(np.ones((n, n), bool))
+            s = np.where(keep, scale * (Q @ K.T), 0.0)
+            e = np.where(keep, (d + 8) * U * scale * (np.abs(Q) @ np.abs(K.T)), 0.0)           # of a score
+            far = 4 * U * (np.abs(s) + np.abs(s).max(axis=1, keepdims=True))                   # of an exponent
+            total = (n / 8 + 32) * U                                                           # of a sum of exponentials
+            E_lse[i, a:b] = (e + far).max(axis=1) + total + 4 * U * np.abs(lse)
+            rp = e + far + (e + far).max(axis=1, keepdims=True) + total
+            aV, aD, aK, aQ = np.abs(V), np.abs(D), np.abs(K), np.abs(Q)
+            o = p @ V
+            E_o[a:b, i] = (p * (h + 2 * rp) + tiny * keep) @ aV + (n + 8) * U * (p @ aV)
+            E_out = E_o[a:b, i] * (1 + h) + h * np.abs(o) + tiny
+            delta, dP = np.sum(D * o, axis=1, keepdims=True), D @ V.T
+            E_delta = np.sum(aD * E_out, axis=1, keepdims=True) + (d + 8) * U * np.sum(aD * np.abs(o), axis=1, keepdims=True)
+            E_dP = (d + 8) * U * (aD @ aV.T)
+            rq = e + far + E_lse[i, a:b, None] + 4 * U * np.abs(lse)[:, None] + 8 * U
+            dS = p * (dP - delta)
+            E_dS = p * (1 + 2 * rq) * (E_dP + E_delta + U * (np.abs(dP) + np.abs(delta))) + 2 * rq * np.abs(dS)
+            E_dS = np.where(keep, E_dS + h * (np.abs(dS) + E_dS) + tiny, 0.0)
+            sums = (n * heads // kv + 8) * U
+            E_g[a:b, i] += scale * (E_dS @ aK + sums * (np.abs(dS) @ aK))
+            E_g[a:b, heads + j] += scale * (E_dS.T @ aQ + sums * (np.abs(dS).T @ aQ))
+            E_g[a:b, heads + kv + j] += (p * (h + 2 * rq) + tiny * keep).T @ aD + sums * (p.T @ aD)
+    return E_o.reshape(T, -1), E_lse, E_g.reshape(T, -1)
+
+
+class Attention:
+    """Operands of a call on sequences of `lens` rows with `front` rows of nobody's in front of them and `pad` behind."""
+
+    def __init__(self, rng, lens, heads, kv, d, front=0, pad=0, extra=0, shift=0, std=1.0, scale=None):
+        import torch
+        self.heads, self.kv, self.d, self.n = heads, kv, d, len(lens)
+        self.offsets = front + np.concatenate([[0], np.cumsum(lens)])
+        self.T = T = int(self.offsets[-1]) + pad
+        self.scale = float(np.float32(d ** -0.5 if scale is None else scale))
+        self.width, self.width_o = (heads + 2 * kv) * d, heads * d
+        self.ld, self.ld_o = self.width + extra, self.width_o + extra
+        self.inside = np.zeros(T, bool)
+        self.inside[front:self.offsets[-1]] = True
+        self.values, self.dvalues = normal(rng, T, self.width, std=std), normal(rng, T, self.width_o)
+        self.qkv = surrounded(T, self.width, self.ld, shift, self.values, self.inside)
+        self.dout = surrounded(T, self.width_o, self.ld_o, shift, self.dvalues, self.inside)
+        self.o, self.dqkv = Padded(T, self.width_o, self.ld_o, shift), Padded(T, self.width, self.ld, shift)
+        self.lse = torch.full((heads, T), 7.0, device="cuda")
+        self.off_dev = dev_i32(self.offsets)
+        self.plan = workspace(B.axonn_attention_packed_plan_bytes(T, self.n))
+        self.ws = workspace(B.axonn_attention_packed_bwd_workspace(T, self.n, heads, kv, d))
+
+    def run(self, stream=None, backward=True):
+        shape = (self.T, self.n, self.heads, self.kv, self.d, self.scale, self.plan, self.qkv.t, self.ld)
+        B.axonn_attention_packed_plan(self.T, self.n, self.off_dev, self.plan, stream)
+        B.axonn_attention_packed_fwd(*shape, self.o.t, self.ld_o, self.lse, stream)
+        if backward:
+            B.axonn_attention_packed_bwd(*shape, self.o.t, self.ld_o, self.lse, self.dout.t, self.ld_o, self.dqkv.t, self.ld, self.ws, stream)
+
+    def results(self):
+        """o, lse, dqkv on the host; checks that rows of nobody's are as they were."""
+        o, lse, g = self.o.result(), host(self.lse), self.dqkv.result()
+        assert (o[~self.inside] == 7).all() and (lse[:, ~self.inside] == 7).all() and (g[~self.inside] == 7).all()
+        return o[self.inside], lse[:, self.inside], g[self.inside]
+
+    def check(self):
+        args = (self.offsets, self.heads, self.kv, self.d, self.scale)
+        x, dy = (np.where(self.inside[:, None], a, 0.0) for a in (self.values, self.dvalues))
+        o_ref, lse_ref = P.packed_attention_fwd(x, *args)
+        g_ref = P.packed_attention_bwd(x, dy, *args)
+        E_o, E_lse, E_g = attention_bounds(x, dy, *args)
+        o, lse, g = self.results()
+        keep = self.inside
+        within(o, o_ref[keep], E_o[keep], label="o")
+        assert (np.abs(lse - lse_ref[:, keep]) <= E_lse[:, keep]).all(), np.abs(lse - lse_ref[:, keep]).max()
+        within(g, g_ref[keep], E_g[keep], label="dqkv")
+
+
+CASES = [
+    # lens, heads, kv, d, front, pad, extra columns, first element
+    ([1], 1, 1, 4, 0, 0, 0, 0), ([1, 2, 3], 2, 1, 8, 0, 0, 0, 0), ([5], 3, 3, 64, 2, 3, 5, 1),
+    ([64, 65, 127, 128, 129, 1], 2, 1, 64, 0, 0, 0, 0), ([0, 5, 0, 300, 0], 4, 2, 128, 0, 7, 0, 0), ([200, 31], 3, 3, 188, 1, 0, 3, 1),
+    ([257, 33], 4, 1, 192, 0, 0, 0, 0), ([130, 1, 1, 62], 8, 8, 80, 3, 3, 3, 1), ([513], 4, 2, 128, 0, 0, 8, 0), ([700], 2, 2, 64, 0, 1, 0, 0),
+    ([33] * 9, 6, 3, 36, 0, 0, 1, 3), ([1] * 70, 4, 4, 32, 0, 0, 0, 0),
+    # more tiles than the one-launch backward takes
+    ([140] * 9 + [3], 16, 4, 128, 0, 5, 0, 0), ([140] * 9 + [300], 16, 16, 64, 0, 0, 0, 0), ([129] * 9, 16, 2, 188, 0, 0, 0, 0),
+    ([131] * 9, 16, 8, 92, 0, 0, 2, 1), ([400, 300, 200, 100, 50, 20, 10, 1] * 2, 8, 1, 64, 0, 0, 0, 0), ([90] * 18, 24, 24, 40, 0, 0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("lens,heads,kv,d,front,pad,extra,shift", CASES)
+def test_attention(lens, heads, kv, d, front, pad, extra, shift):
+    a = Attention(np.random.default_rng(sum(lens) + d), lens, heads, kv, d, front, pad, extra, shift)
+    a.run()
+    a.check()
+    first = [x.clone() for x in (a.o.t, a.lse, a.dqkv.t)]
+    a.dqkv.t[:] = 7
+    a.run()
+    a.results()
+    assert all((x == y).all() for x, y in zip(first, (a.o.t, a.lse, a.dqkv.t))), "another result the second time"
+
+
+@pytest.mark.parametrize("d,heads,kv", [(64, 4, 2), (128, 2, 1), (188, 2, 2)])
+@pytest.mark.parametrize("std,scale", [(4.0, None), (1.0, 3.0), (0.01, 1e-3)])
+def test_attention_of_steep_and_flat_scores(d, heads, kv, std, scale):
+    a = Attention(np.random.default_rng(5), [300, 77, 1], heads, kv, d, std=std, scale=scale)
+    a.run()
+    a.check()
+
+
+@pytest.mark.parametrize("heads,kv,d", [(4, 2, 128), (16, 8, 64)])
+def test_a_sequence_does_not_depend_on_its_neighbours(heads, kv, d):
+    """The same bits wherever a sequence lies and whatever the others hold, infinities and NaN too."""
+    import torch
+    rng = np.random.default_rng(8)
+    lens = [150, 260, 150, 97, 260]
+    a = Attention(rng, lens, heads, kv, d)
+    off = a.offsets
+    same = [(0, 2), (1, 4)]
+    for m in (a.qkv, a.dout):
+        for i, j in same:
+            m.t[off[j]:off[j + 1]] = m.t[off[i]:off[i + 1]]
+    m = a.qkv.t
+    bad = slice(int(off[3]), int(off[4]))
+    outs = []
+    for value in (1.0, float("nan"), float("inf")):
+        m[bad] = value
+        a.run()
+        outs.append([x.clone() for x in (a.o.t, a.lse.t(), a.dqkv.t)])
+    good = torch.ones(a.T, dtype=torch.bool)
+    good[bad] = False
+    for out in outs:
+        for x, y in zip(outs[0], out):
+            assert (x[good] == y[good]).all() and torch.isfinite(x[good]).all()
+            for i, j in same:
+                assert (y[off[i]:off[i + 1]] == y[off[j]:off[j + 1]]).all()
+
+
+def test_attention_rows_beyond_32_bit_offsets():
+    """Sequences whose rows lie more than 2^31 elements behind the first row."""
+    import torch
+    heads, kv, d, T, ld = 2, 1, 64, 1200, 1 << 21
+    rng = np.random.default_rng(11)
+    lens = [20, 900, 150, 130]
+    a = Attention(rng, lens, heads, kv, d)
+    big = torch.empty(T * ld, dtype=B.torch_elem_dtype(), device="cuda").view(T, ld)
+    out = torch.empty(T * ld, dtype=B.torch_elem_dtype(), device="cuda").view(T, ld)
+    big[:, :a.width], big[:, 4096:4096 + a.width_o] = a.qkv.t, a.dout.t
+    a.run()
+    shape = (T, a.n, heads, kv, d, a.scale, a.plan, big, ld)
+    o, dout, dqkv, lse = out[:, 4096:], big[:, 4096:], out, torch.zeros_like(a.lse)
+    B.axonn_attention_packed_fwd(*shape, o, ld, lse)
+    B.axonn_attention_packed_bwd(*shape, o, ld, lse, dout, ld, dqkv, ld, a.ws)
+    assert (o[:, :a.width_o] == a.o.t).all() and (lse == a.lse).all() and (dqkv[:, :a.width] == a.dqkv.t).all()
+
+
+@pytest.mark.parametrize("T,offsets", [
+    (1, [0, 1]), (300, [0, 300]), (1000, [0, 0, 128, 256, 257, 1000, 1000]), (900, [5, 3, 400, 200, 901, 7]), (900, [-7, 20, 2000]),
+    (100000, "many"), (1 << 24, [0, 1 << 24]), (1 << 24, [0, 1 << 20, 1 << 23, (1 << 24) - 5]), (70, [70, 70])])
+def test_plan(T, offsets):
+    """Every tile of every sequence once, those with the most tiles in front of them first (as far as these are told apart)."""
+    rng = np.random.default_rng(3)
+    if offsets == "many":
+        offsets = np.sort(rng.integers(0, T + 1, 5001))
+    n = len(offsets) - 1
+    plan = workspace(B.axonn_attention_packed_plan_bytes(T, n))
+    B.axonn_attention_packed_plan(T, n, dev_i32(offsets), plan)
+    got = plan.cpu().numpy().view(np.int32)
+    want = [(a, b - a, t, 0) for a, b in P.sequences(offsets, T) for t in range((b - a + 127) // 128)]
+    assert got[0] == len(want) <= T // 128 + n
+    items = got[4:4 + 4 * len(want)].reshape(-1, 4)
+    assert sorted(map(tuple, items.tolist())) == sorted(want)
+    assert (np.diff(np.minimum(items[:, 2], 4095)) <= 0).all()
+
+
+def test_attention_with_disordered_offsets():
+    """Offsets that do not ascend: the sequences that the header says they stand for, nothing written elsewhere."""
+    rng = np.random.default_rng(2)
+    a = Attention(rng, [100, 0, 60, 40], 2, 2, 64, pad=10)
+    a.off_dev = dev_i32([0, 100, 30, 160, 200])            # the third is taken as the second
+    a.run()
+    a.check()
+
+
+def test_a_list_that_is_no_plan_leaves_the_rows():
+    """Whatever the plan's memory holds, no workgroup reads or writes outside the T rows."""
+    import torch
+    rng = np.random.default_rng(2)
+    a = Attention(rng, [100, 60], 2, 2, 64)
+    a.run()
+    items = a.plan.view(torch.int32)
+    items[4:] = torch.tensor([150, 60, 0, 0, -5, 20, 0, 0, 10, -1, 0, 0], dtype=torch.int32, device="cuda")
+    shape = (a.T, a.n, a.heads, a.kv, a.d, a.scale, a.plan, a.qkv.t, a.ld)
+    a.o.t[:] = 7
+    B.axonn_attention_packed_fwd(*shape, a.o.t, a.ld_o, a.lse)
+    B.axonn_attention_packed_bwd(*shape, a.o.t, a.ld_o, a.lse, a.dout.t, a.ld_o, a.dqkv.t, a.ld, a.ws)
+    assert (a.o.result() == 7).all()
+
+
+def test_attention_captured_with_other_sequences_at_each_replay():
+    import torch
+    rng = np.random.default_rng(9)
+    packs = [Attention(rng, lens, 4, 2, 64, pad=pad) for lens, pad in (([100, 200, 84], 16), ([1, 300, 99], 0), ([0, 0, 390], 10), ([133, 133, 133], 1))]
+    a = packs[0]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        a.run(stream)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        a.run(stream)
+    for p in packs + packs[:2]:
+        p.run()
+        a.qkv.t.copy_(p.qkv.t)
+        a.dout.t.copy_(p.dout.t)
+        a.off_dev.copy_(p.off_dev)
+        graph.replay()
+        torch.cuda.synchronize()
+        keep = torch.from_numpy(p.inside).cuda()
+        assert all((x[keep] == y[keep]).all() for x, y in zip((a.o.t, a.lse.t(), a.dqkv.t), (p.o.t, p.lse.t(), p.dqkv.t)))
+
+
+def test_attention_on_two_streams_at_once():
+    import torch
+    rng = np.random.default_rng(10)
+    calls = [Attention(rng, [300, 500, 90], 16, 4, 128), Attention(rng, [200] * 6, 8, 8, 64)]
+    want = []
+    for a in calls:
+        a.run()
+        want.append([x.clone() for x in (a.o.t, a.lse, a.dqkv.t)])
+        for x in (a.o.t, a.lse, a.dqkv.t):
+            x[:] = 0
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        for a, s in zip(calls, streams):
+            a.run(s)
+    torch.cuda.synchronize()
+    for a, w in zip(calls, want):
+        assert all((x == y).all() for x, y in zip((a.o.t, a.lse, a.dqkv.t), w))

@@ -1,0 +1,119 @@
+"""What the operations on packed sequences refuse, and with which status: checked on the host, in front of any launch; the sizes are
+those that the header names."""
+import pytest
+
+from paper_2110_13005_amd import binding as B
+from test_step_ops_limits import comment_of
+from test_step_ops_refusals import A, INV, UNS, refused, with_args
+
+
+def nulls(fn, ok, positions):
+    for pos in positions:
+        refused(INV, fn, *with_args(ok, **{"_%d" % pos: None}))
+
+
+def each(status, fn, ok, changes):
+    for pos, values in changes.items():
+        for v in values:
+            refused(status, fn, *with_args(ok, **{"_%d" % pos: v}))
+
+
+def test_plan():
+    for fn, ok in ((B.axonn_attention_packed_plan, [40, 3, A, A]), (B.axonn_attention_packed_plan_bytes, [40, 3])):
+        each(INV, fn, ok, {0: (0, -1), 1: (0, -1)})
+        each(UNS, fn, ok, {0: ((1 << 24) + 1,), 1: ((1 << 20) + 1,)})
+    nulls(B.axonn_attention_packed_plan, [40, 3, A, A], (2, 3))
+    refused(INV, B.axonn_attention_packed_plan, 40, 3, A, A + 8)
+    assert B.load().axonn_attention_packed_plan_bytes(40, 3, None) == INV
+    assert "T <= 2^24, n_seq <= 2^20" in comment_of("axonn_attention_packed_plan_bytes")
+    # every sequence's last tile may hold one row
+    assert B.axonn_attention_packed_plan_bytes(1000, 5) >= 16 * (1000 // 128 + 5)
+
+
+SHAPE = [300, 2, 8, 2, 64, 0.125]
+WIDTH, WIDTH_O = (8 + 4) * 64, 8 * 64
+
+
+def shapes(fn, ok):
+    each(INV, fn, ok, {0: (0,), 1: (0,), 2: (0, -8), 3: (0, 3, 16), 4: (0, -4), 5: (0.0, -1.0, float("nan"), float("inf"))})
+    each(UNS, fn, ok, {0: ((1 << 24) + 1,), 4: (62, 196, 256)})
+    refused(UNS, fn, *with_args(ok, _2=4098))
+    refused(UNS, fn, *with_args(ok, _0=(1 << 24) + 8 - 8, _2=16))             # 2^28 rows times heads
+    refused(UNS, fn, *with_args(ok, _1=1 << 20, _2=16))
+
+
+def test_attention_forward():
+    ok = SHAPE + [A, A, WIDTH, A + 4096, WIDTH_O, A]
+    fn = B.axonn_attention_packed_fwd
+    nulls(fn, ok, (6, 7, 9, 11))
+    shapes(fn, ok)
+    each(INV, fn, ok, {8: (WIDTH - 1,), 10: (WIDTH_O - 1,), 6: (A + 4,), 11: (A + 2,), 9: (A,)})
+    each(UNS, fn, ok, {8: ((1 << 22) + 1,), 10: ((1 << 22) + 1,)})
+    text = comment_of("axonn_attention_packed_fwd")
+    for limit in ("head_dim a multiple of 4, at most 192", "at most 4096", "T * n_heads <= 2^27", "n_seq * n_heads <= 2^23",
+                  "leading dimensions at most 2^22"):
+        assert limit in text, limit
+
+
+def test_attention_backward():
+    ok = SHAPE + [A, A, WIDTH, A + 4096, WIDTH_O, A, A + 8192, WIDTH_O, A + 12288, WIDTH, A]
+    fn = B.axonn_attention_packed_bwd
+    nulls(fn, ok, (6, 7, 9, 11, 12, 14, 16))
+    shapes(fn, ok)
+    each(INV, fn, ok, {8: (WIDTH - 1,), 10: (WIDTH_O - 1,), 13: (WIDTH_O - 1,), 15: (WIDTH - 1,), 6: (A + 8,), 16: (A + 8,), 11: (A + 2,)})
+    each(INV, fn, ok, {14: (A, A + 4096, A + 8192)})                           # over qkv, o, dout
+    each(UNS, fn, ok, {8: ((1 << 22) + 1,), 13: ((1 << 22) + 1,), 15: ((1 << 22) + 1,)})
+    assert B.load().axonn_attention_packed_bwd_workspace(300, 2, 8, 2, 64, None) == INV
+    shapes_of = [300, 2, 8, 2, 64]
+    each(INV, B.axonn_attention_packed_bwd_workspace, shapes_of, {0: (0,), 3: (3,), 4: (0,)})
+    assert B.axonn_attention_packed_bwd_workspace(*shapes_of) >= 4 * 300 * 8
+
+
+def logits(fn, ok, T=0, V=1, ld=3):
+    each(INV, fn, ok, {T: (0, -1), V: (0, -1)})
+    if ld is not None:
+        refused(INV, fn, *with_args(ok, **{"_%d" % ld: ok[V] - 1}))
+    refused(UNS, fn, *with_args(ok, **{"_%d" % T: (1 << 22) + 1}))
+    refused(UNS, fn, *with_args(ok, **({"_%d" % V: (1 << 20) + 1, "_%d" % ld: 1 << 21} if ld is not None else {"_%d" % V: (1 << 20) + 1})))
+
+
+def test_token_logprobs():
+    ok = [4, 10, A, 10, A, A, A]
+    nulls(B.axonn_token_logprobs_fwd, ok, (2, 4, 5, 6))
+    logits(B.axonn_token_logprobs_fwd, ok)
+    ok = [4, 10, A, 10, A, A, A, A, 10]
+    nulls(B.axonn_token_logprobs_bwd, ok, (2, 4, 5, 6, 7))
+    logits(B.axonn_token_logprobs_bwd, ok)
+    each(INV, B.axonn_token_logprobs_bwd, ok, {8: (9, 11)})                    # too small; in place with another one
+    assert "T <= 2^22, V <= 2^20" in comment_of("axonn_token_logprobs_fwd")
+
+
+def test_policy_loss():
+    ok = [4, 10, A, 10, A, A, A, A, A, 0.2, 0.2, 0.1, 1.0, A, A, A, A, 10]
+    fn = B.axonn_policy_loss
+    nulls(fn, ok, (2, 4, 5, 6, 7, 8, 14))
+    logits(fn, ok)
+    bad = (float("nan"), float("inf"), -0.1)
+    each(INV, fn, ok, {9: bad + (1.5,), 10: bad, 11: bad, 12: bad + (0.0,), 17: (9, 11)})
+
+
+def test_preference_loss():
+    ok = [40, 2, 10, A, A, A, A, 0.1, 0.1, 1.0, 1.0, A, A, A]
+    fn = B.axonn_preference_loss
+    nulls(fn, ok, (3, 4, 5, 11, 13))
+    logits(fn, ok, V=2, ld=None)
+    bad = (float("nan"), float("inf"), -0.1)
+    each(INV, fn, ok, {1: (0, -1), 7: bad + (0.0,), 8: bad + (1.1,), 9: bad + (0.0,), 10: bad + (0.0,)})
+    refused(UNS, fn, *with_args(ok, _1=(1 << 19) + 1))
+
+
+def test_distill_loss():
+    ok = [4, 100, 8, A, 100, A, A, 8, A, 1.0, A, 1.0, A, A, A, 100]
+    fn = B.axonn_distill_loss
+    nulls(fn, ok, (3, 5, 6, 10, 12))
+    logits(fn, ok, ld=4)
+    bad = (float("nan"), float("inf"), -1.0, 0.0)
+    each(INV, fn, ok, {2: (0, -1), 7: (7,), 9: bad + (1e-40,), 11: bad, 15: (99, 101)})
+    refused(UNS, fn, *with_args(ok, _2=1025, _7=1025))
+    refused(UNS, fn, *with_args(ok, _1=393217, _4=393217, _15=393217))
+    assert "K <= 1024, V <= 393216" in comment_of("axonn_distill_loss")
