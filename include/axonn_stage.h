@@ -673,8 +673,8 @@ int axonn_preference_loss(int64_t T, int32_t n_pairs, int64_t V, const int32_t* 
  *                      Q = the student's mass of the tokens that are not named
  *   loss[0] = sum_t weight[t] token_loss[t],   dlogits = loss_scale d loss / d logits
  * A token named twice counts as two entries.  Rows in which no token is named, or whose weight is 0, have
- * no part: token_loss 0, dlogits zeros (the logits are not read).  loss may be NULL; so may dlogits, or it
- * may be logits.  K <= 1024, V <= 393216. */
+ * no part: token_loss 0, dlogits zeros.  loss may be NULL; so may dlogits, or it
+ * may be logits.  K <= 1024, V <= 393216, temperature in [2^-16, 2^16]. */
 int axonn_distill_loss(int64_t T, int64_t V, int32_t K, const void* logits_bf16, int64_t ld_logits,
                        const float* teacher_logits, const int32_t* teacher_ids, int64_t ld_teacher,
                        const float* teacher_lse, float temperature, const float* weight,

@@ -3,100 +3,284 @@
 //
 // With q = softmax(z), every gradient is a multiple of q plus a few elements of its own:
 //   d log q_t / dz = onehot_t - q
-// A row's maximum and sum of exponentials come from one sweep with the running-maximum recurrence.  Tokens without a part are not read.
+// HBM-bound: a row of logits is read once and its gradient written once.  A workgroup holds the row in registers between the two (vocabularies
+// of up to 65536; longer rows are read twice).  Tokens without a part are not read.
 #include "rows.h"
+#include "host_logic.h"
+#include <type_traits>
 
 namespace axonn {
 
-constexpr int LOSS_THREADS = 256;
+constexpr float kLog2eLoss = 1.4426950408889634f;
 
-// exp(x c) of the difference of two logits; c = log2(e) / temperature.  (The difference is taken first: the product of a logit of
-// the type's lowest value with c alone would be infinite.)
-__device__ __forceinline__ float exp_scaled(float x, float c) { return __builtin_amdgcn_exp2f(x * c); }
-
+struct OpMax {
+  static constexpr float none = -INFINITY;
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct OpSum {
+  static constexpr float none = 0.f;
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+// op over the 64 lanes of a wave, in all of them (a scalar): shifts inside rows of 16 lanes, then row 0 to 1 and 2 to 3, then the
+// lower half to the upper one.  The data path of the vector unit, no LDS round trips.
+template <class Op>
+__device__ __forceinline__ float wave_all(float v, Op op) {
+  const auto from = [&](auto ctrl, auto rows) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(Op::none), __float_as_uint(v), decltype(ctrl)::value, decltype(rows)::value,
+                                                       0xf, false));
+  };
+  using std::integral_constant;
+  v = op(v, from(integral_constant<int, 0x111>(), integral_constant<int, 0xf>()));
+  v = op(v, from(integral_constant<int, 0x112>(), integral_constant<int, 0xf>()));
+  v = op(v, from(integral_constant<int, 0x114>(), integral_constant<int, 0xf>()));
+  v = op(v, from(integral_constant<int, 0x118>(), integral_constant<int, 0xf>()));
+  v = op(v, from(integral_constant<int, 0x142>(), integral_constant<int, 0xa>()));
+  v = op(v, from(integral_constant<int, 0x143>(), integral_constant<int, 0xc>()));
+  return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63));
+}
+// op over all threads of a workgroup, in all of them; `shared` is used for nothing else.
 template <int THREADS, class Op>
-__device__ __forceinline__ float block_all(float v, float* shared, Op op) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o, 64));
-  __syncthreads();
+__device__ __forceinline__ float block_all(float v, float (&shared)[THREADS / 64], Op op) {
+  v = wave_all(v, op);
   if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = shared[0];
+  const int lane = threadIdx.x & 63;
+  return wave_all(lane < THREADS / 64 ? shared[lane] : Op::none, op);
+}
+
+// exp((z - m) / temperature) as exp2(z c - m c) with c = log2(e) / temperature: one fused multiply-add and one exponential.  m c is
+// rounded; every exponential of the row is off by the same factor 2^low, which cancels in the softmax and is taken out of the
+// logarithm of their sum.  Where m c comes near the largest number (a bfloat16 row whose maximum is about the type's largest or, with
+// nothing else in it, lowest value) other values than m lie so far below it that any c gives them 0: a power of two, with which
+// that of m is exact.
+struct Exponent {
+  float c, m, mc, low;
+  // from the maximum m, the same in all lanes; of nothing but -inf (or NaN, which has to stay) from 0
+  __device__ __forceinline__ Exponent(float m_, float c_) {
+    m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m_ == -INFINITY ? 0.f : m_)));
+    c = fabsf(m) * c_ < 0x1p126f ? c_ : 0x1p-30f;
+    mc = m * c;
+    low = m == INFINITY ? 0.f : fmaf(m, c, -mc);
+  }
+  __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, c, -mc)); }
+  // log of the sum of exp((z - m) / temperature) from the sum of these
+  __device__ __forceinline__ float log_of(float sum) const { return logf(sum) - low * 0.6931471805599453f; }
+};
+
+// Maximum and sum of exponentials of a row, in all threads; `shared` for the two reductions.
+template <int THREADS>
+struct RowShared { float max[THREADS / 64], sum[THREADS / 64]; };
+struct RowStats { Exponent e; float sum; };
+
+// The chunk of a row that a lane takes as 16 bytes, or its last, shorter one; -inf behind the row (n <= 0: all of it).
+__device__ __forceinline__ elemx8 logits_chunk(const elem_t* p, int n) {
+  if (n >= 8) return *reinterpret_cast<const elemx8_any*>(p);
+  elemx8 v;
 #pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) v = op(v, shared[w]);
+  for (int i = 0; i < 8; ++i) v[i] = (elem_t)-INFINITY;
+#pragma unroll
+  for (int i = 0; i < 7; ++i)
+    if (i < n) v[i] = p[i];
   return v;
 }
-struct OpMax { __device__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-struct OpSum { __device__ float operator()(float a, float b) const { return a + b; } };
-
-// Maximum m of a row's logits and sum of exp((z - m) c) in all threads.
-struct RowStats { float m, sum; };
-// What exponentials are taken from: the maximum, or 0 where nothing but -inf (or NaN, which has to stay) has been seen.
-__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ void stats_add(RowStats& s, const elemx8& v, int n, float c) {
-  const float old = s.m;
-  float top = -INFINITY;
+// -inf for the elements whose bits are set
+__device__ __forceinline__ void leave_out(elemx8& v, uint32_t bits) {
+  if (bits == 0) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (i < n) top = fmaxf(top, (float)v[i]);
-  s.m = fmaxf(s.m, top);
-  const float m = reference(s.m);
-  float part = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (i < n) part += exp_scaled((float)v[i] - m, c);
-  s.sum = s.sum * exp_scaled(old - m, c) + part;
+    if (bits >> i & 1) v[i] = (elem_t)-INFINITY;
 }
-template <int THREADS>
-__device__ __forceinline__ RowStats stats_join(RowStats s, float c, float* shared) {
-  const float m = block_all<THREADS>(s.m, shared, OpMax());
-  return RowStats{m, block_all<THREADS>(s.sum * exp_scaled(s.m - reference(m), c), shared, OpSum())};
+__device__ __forceinline__ float chunk_max(float m, const elemx8& v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, (float)v[i]);
+  return m;
+}
+// f times the exponentials of a chunk
+__device__ __forceinline__ elemx8 chunk_gradient(const elemx8& v, const Exponent& e, float f) {
+  elemx8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (elem_t)(e((float)v[i]) * f);
+  return r;
+}
+// Chunk number `chunk` of a row: a base that is the same in all lanes and 32 bits of offset.
+template <class T>
+__device__ __forceinline__ T* chunk_of(T* row, uint32_t chunk) {
+  return (T*)((char*)const_cast<elem_t*>(row) + chunk * 16u);
 }
 
-constexpr float kLog2e_ = 1.4426950408889634f;
-
-// dlogits[v] = slope (onehot_t - q) for the whole row; slope 0: zeros, and the row is not read.
-__device__ __forceinline__ void write_gradient(const elem_t* row, elem_t* out, int V, int target, RowStats s, float slope, int tid) {
-  const float f = -slope / s.sum;
-  for (int c = tid * 8; c < V; c += LOSS_THREADS * 8) {
-    elemx8 r = {};
-    if (slope != 0.f) {
-      const elemx8 v = load_chunk(row + c, V - c);
+// A row of logits in the registers of a workgroup: thread t of THREADS holds chunks t, t + THREADS, ... of 8, as many as it takes
+// (so all but the last, or the last two where there is no kernel for every number, are whole: the first WHOLE).
+constexpr int row_whole(int chunks) { return chunks <= 8 ? chunks - 1 : chunks - 2; }
+template <int THREADS, int CHUNKS, int WHOLE = row_whole(CHUNKS)>
+struct Row {
+  elemx8 v[CHUNKS];
+  __device__ __forceinline__ void load(const elem_t* row, int V, int tid) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = (elem_t)(exp_scaled((float)v[i] - s.m, kLog2e_) * f + (c + i == target ? slope : 0.f));
+    for (int j = 0; j < CHUNKS; ++j) {
+      const uint32_t chunk = tid + j * THREADS;
+      v[j] = logits_chunk(chunk_of(row, chunk), j < WHOLE ? 8 : V - 8 * (int)chunk);
     }
-    store_chunk(out + c, r, V - c);
   }
+  // The elements are converted anew in every sweep: kept converted they would take twice the registers.
+  __device__ __forceinline__ void anew() {
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) asm volatile("" : "+v"(v[j]));
+  }
+  // without the tokens whose bits are set
+  __device__ __forceinline__ void without(const uint8_t* named, int V, int tid) {
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+      const int chunk = tid + j * THREADS;
+      if ((j < WHOLE) || 8 * chunk < V) leave_out(v[j], named[chunk]);
+    }
+  }
+  __device__ __forceinline__ float sum(const Exponent& e) {
+    anew();
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+      float part = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part += e((float)v[j][i]);
+      s += part;
+    }
+    return s;
+  }
+  __device__ __forceinline__ RowStats stats(float c, RowShared<THREADS>& shared) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) m = chunk_max(m, v[j]);
+    const Exponent e(block_all<THREADS>(m, shared.max, OpMax()), c);
+    return RowStats{e, block_all<THREADS>(sum(e), shared.sum, OpSum())};
+  }
+  // f times the exponentials
+  __device__ __forceinline__ void store(elem_t* out, int V, int tid, const Exponent& e, float f) {
+    anew();
+#pragma unroll
+    for (int j = 0; j < CHUNKS; ++j) {
+      const uint32_t chunk = tid + j * THREADS;
+      const int n = j < WHOLE ? 8 : V - 8 * (int)chunk;
+      if (n > 0) store_chunk(chunk_of(out, chunk), chunk_gradient(v[j], e, f), n);
+    }
+  }
+  // of one element more, by the thread that has stored its chunk
+  __device__ __forceinline__ static void store_one(elem_t* out, int tid, int column, float value) {
+    if (tid == (column >> 3) % THREADS) out[column] = (elem_t)value;
+  }
+};
+// A row that is too long for them: read for its statistics, with the running-maximum recurrence, and once more for the gradient.
+template <int THREADS>
+struct Row<THREADS, 0, -1> {
+  static constexpr int AT_ONCE = 4;
+  const elem_t* row;
+  const uint8_t* named;
+  int V, tid;
+  __device__ __forceinline__ void load(const elem_t* row_, int V_, int tid_) { row = row_; V = V_; tid = tid_; named = nullptr; }
+  __device__ __forceinline__ void without(const uint8_t* named_, int, int) { named = named_; }
+  __device__ __forceinline__ void chunks(int first, elemx8 (&v)[AT_ONCE]) const {
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int at = first + 8 * j * THREADS;
+      v[j] = logits_chunk(row + at, V - at);
+    }
+    if (named) {
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const int at = first + 8 * j * THREADS;
+        if (at < V) leave_out(v[j], named[at >> 3]);
+      }
+    }
+  }
+  __device__ __forceinline__ RowStats stats(float c, RowShared<THREADS>& shared) const {
+    float m = -INFINITY, sum = 0.f;
+    for (int at = 8 * tid; at < V; at += 8 * THREADS * AT_ONCE) {
+      elemx8 v[AT_ONCE];
+      chunks(at, v);
+      const float old = m;
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) m = chunk_max(m, v[j]);
+      const float from = m == -INFINITY ? 0.f : m;
+      float part = 0.f;
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part += __builtin_amdgcn_exp2f(((float)v[j][i] - from) * c);
+      sum = sum * __builtin_amdgcn_exp2f((old - from) * c) + part;
+    }
+    const Exponent e(block_all<THREADS>(m, shared.max, OpMax()), c);
+    sum = block_all<THREADS>(sum * __builtin_amdgcn_exp2f((m - e.m) * c), shared.sum, OpSum());
+    return RowStats{e, sum * __builtin_amdgcn_exp2f(e.low)};
+  }
+  __device__ __forceinline__ void store(elem_t* out, int, int, const Exponent& e, float f) const {
+    for (int first = 8 * tid; first < V; first += 8 * THREADS * AT_ONCE) {
+      elemx8 v[AT_ONCE];
+      chunks(first, v);
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const int at = first + 8 * j * THREADS;
+        if (at >= V) continue;
+        store_chunk(out + at, chunk_gradient(v[j], e, f), V - at);
+      }
+    }
+  }
+  __device__ __forceinline__ static void store_one(elem_t* out, int tid, int column, float value) {
+    if (tid == (column >> 3) % THREADS) out[column] = (elem_t)value;
+  }
+};
+template <int THREADS>
+__device__ __forceinline__ void store_zeros(elem_t* out, int V, int tid) {
+  const elemx8 zero = {};
+  for (int c = tid * 8; c < V; c += THREADS * 8) store_chunk(out + c, zero, V - c);
 }
 
-__global__ __launch_bounds__(LOSS_THREADS) void token_logprobs_fwd_kernel(int V, const elem_t* __restrict__ logits, int64_t ld,
-                                                                          const int* __restrict__ targets, float* __restrict__ logp,
-                                                                          float* __restrict__ lse) {
-  __shared__ float shared[LOSS_THREADS / 64];
+template <int THREADS, int CHUNKS>
+__global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void token_logprobs_fwd_kernel(int V, const elem_t* __restrict__ logits, int64_t ld,
+                                                                     const int* __restrict__ targets, float* __restrict__ logp,
+                                                                     float* __restrict__ lse) {
+  __shared__ RowShared<THREADS> shared;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, target = targets[t];
   if (target < 0 || target >= V) {
     if (tid == 0) logp[t] = lse[t] = 0.f;
     return;
   }
-  const elem_t* row = logits + t * ld;
-  RowStats s{-INFINITY, 0.f};
-  for (int c = tid * 8; c < V; c += LOSS_THREADS * 8) stats_add(s, load_chunk(row + c, V - c), V - c, kLog2e_);
-  s = stats_join<LOSS_THREADS>(s, kLog2e_, shared);
+  Row<THREADS, CHUNKS> row;
+  row.load(logits + t * ld, V, tid);
+  const float at_target = (float)logits[t * ld + target];
+  const RowStats s = row.stats(kLog2eLoss, shared);
   if (tid == 0) {
-    const float log_sum = logf(s.sum);
-    logp[t] = ((float)row[target] - s.m) - log_sum;
-    lse[t] = s.m + log_sum;
+    const float log_sum = s.e.log_of(s.sum);
+    logp[t] = (at_target - s.e.m) - log_sum;
+    lse[t] = s.e.m + log_sum;
   }
 }
 
-__global__ __launch_bounds__(LOSS_THREADS) void token_logprobs_bwd_kernel(int V, const elem_t* logits, int64_t ld,
-                                                                          const int* __restrict__ targets, const float* __restrict__ lse,
-                                                                          const float* __restrict__ dlogp, elem_t* dlogits, int64_t ld_d) {
-  const int64_t t = blockIdx.x;
-  const int target = targets[t];
+// A workgroup takes so many chunks per thread of a row.
+constexpr int GRAD_THREADS = 256;
+template <int CHUNKS>
+__global__ __launch_bounds__(GRAD_THREADS) void token_logprobs_bwd_kernel(int V, uint32_t parts, uint32_t parts_recip, const elem_t* logits,
+                                                                          int64_t ld, const int* __restrict__ targets,
+                                                                          const float* __restrict__ lse, const float* __restrict__ dlogp,
+                                                                          elem_t* dlogits, int64_t ld_d) {
+  constexpr int COLUMNS = 8 * GRAD_THREADS * CHUNKS;
+  const uint32_t t = host::recip_div(blockIdx.x, parts, parts_recip), first = (blockIdx.x - t * parts) * COLUMNS;
+  const int target = targets[t], tid = threadIdx.x, n = min(V - (int)first, COLUMNS);
   const float slope = target < 0 || target >= V ? 0.f : dlogp[t];
-  write_gradient(logits + t * ld, dlogits + t * ld_d, V, target, RowStats{lse[t], 1.f}, slope, threadIdx.x);
+  elem_t* const out = dlogits + t * ld_d + first;
+  if (slope == 0.f) {
+    store_zeros<GRAD_THREADS>(out, n, tid);
+    return;
+  }
+  Row<GRAD_THREADS, CHUNKS, 0> row;
+  row.load(logits + t * ld + first, n, tid);
+  const Exponent e(lse[t], kLog2eLoss);
+  const bool here = target >= (int)first && target < (int)first + n;
+  const float at_target = here ? (float)logits[t * ld + target] : 0.f;
+  if (logits == dlogits) __syncthreads();             // read before it is overwritten
+  // exp(z - lse) with the rounded product's factor taken out
+  const float f = -slope * __builtin_amdgcn_exp2f(-e.low);
+  row.store(out, n, tid, e, f);
+  if (here) row.store_one(out, tid, target - (int)first, e(at_target) * f + slope);
 }
 
 // loss and its derivative by logp
@@ -112,211 +296,257 @@ __device__ __forceinline__ void policy_token(const PolicyArgs& p, float logp, fl
     slope -= p.kl_coef * e;
   }
 }
-__global__ __launch_bounds__(LOSS_THREADS) void policy_loss_kernel(PolicyArgs p) {
-  __shared__ float shared[LOSS_THREADS / 64];
+template <int THREADS, int CHUNKS>
+__global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void policy_loss_kernel(PolicyArgs p) {
+  __shared__ RowShared<THREADS> shared;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, V = p.V, target = p.targets[t];
   const float w = p.weight[t];
-  elem_t* out = (elem_t*)p.dlogits + t * p.ld_d;
+  elem_t* const out = (elem_t*)p.dlogits + t * p.ld_d;
   if (target < 0 || target >= V || w == 0.f) {
     if (tid == 0) {
       p.token_loss[t] = 0.f;
       if (p.logp) p.logp[t] = 0.f;
     }
-    if (p.dlogits) write_gradient(nullptr, out, V, 0, RowStats{0.f, 1.f}, 0.f, tid);
+    if (p.dlogits) store_zeros<THREADS>(out, V, tid);
     return;
   }
-  const elem_t* row = (const elem_t*)p.logits + t * p.ld;
-  const float at_target = (float)row[target];
-  RowStats s{-INFINITY, 0.f};
-  for (int c = tid * 8; c < V; c += LOSS_THREADS * 8) stats_add(s, load_chunk(row + c, V - c), V - c, kLog2e_);
-  s = stats_join<LOSS_THREADS>(s, kLog2e_, shared);
-  const float logp = (at_target - s.m) - logf(s.sum);
+  const elem_t* const logits = (const elem_t*)p.logits + t * p.ld;
+  Row<THREADS, CHUNKS> row;
+  row.load(logits, V, tid);
+  const float at_target = (float)logits[target], old_logp = p.old_logp[t], ref_logp = p.ref_logp ? p.ref_logp[t] : 0.f, A = p.advantage[t];
+  const RowStats s = row.stats(kLog2eLoss, shared);
+  const float logp = (at_target - s.e.m) - s.e.log_of(s.sum);
   float loss, slope;
-  policy_token(p, logp, p.old_logp[t], p.ref_logp ? p.ref_logp[t] : 0.f, p.advantage[t], loss, slope);
+  policy_token(p, logp, old_logp, ref_logp, A, loss, slope);
   if (tid == 0) {
     p.token_loss[t] = loss;
     if (p.logp) p.logp[t] = logp;
   }
-  if (p.dlogits) write_gradient(row, out, V, target, s, slope * w * p.loss_scale, tid);
+  if (!p.dlogits) return;
+  slope *= w * p.loss_scale;
+  if (slope == 0.f) store_zeros<THREADS>(out, V, tid);
+  else {
+    row.store(out, V, tid, s.e, -slope / s.sum);
+    row.store_one(out, tid, target, slope * (1.f - s.e(at_target) / s.sum));
+  }
 }
 
-// One workgroup per pair; the one behind the last clears dlogp of the rows that belong to no sequence.  The sums are long and their
-// difference is what counts: 64 bits.
-__global__ __launch_bounds__(LOSS_THREADS) void preference_loss_kernel(PreferenceArgs p) {
-  __shared__ double shared[2][LOSS_THREADS / 64];
-  const int pair = blockIdx.x, tid = threadIdx.x, T = p.T;
+// The sums of a pair are long and their difference is what counts: 64 bits.  A wave takes a pair; with ALL the workgroup is the only one,
+// takes the pairs in turn and leaves their sum, otherwise it is a pair's and its waves share the tokens.
+constexpr int PREF_THREADS = 1024, PREF_ALONE = 1024;        // rows up to which one workgroup takes all pairs
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+template <bool ALL>
+__global__ __launch_bounds__(PREF_THREADS) void preference_loss_kernel(PreferenceArgs p, float* __restrict__ loss) {
+  constexpr int WAVES = PREF_THREADS / 64, STEP = ALL ? 64 : PREF_THREADS;
+  __shared__ double shared[2][WAVES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = p.T;
   const auto offset = [&](int i) { return min(max(p.offsets[i], 0), T); };
-  if (pair == p.n_pairs) {
-    for (int t = tid; t < offset(0); t += LOSS_THREADS) p.dlogp[t] = 0.f;
-    for (int t = offset(2 * p.n_pairs) + tid; t < T; t += LOSS_THREADS) p.dlogp[t] = 0.f;
-    return;
+  // rows that belong to no sequence: by the workgroup behind the last pair's
+  if (ALL || (int)blockIdx.x == p.n_pairs) {
+    for (int t = tid; t < offset(0); t += PREF_THREADS) p.dlogp[t] = 0.f;
+    for (int t = offset(2 * p.n_pairs) + tid; t < T; t += PREF_THREADS) p.dlogp[t] = 0.f;
+    if (!ALL) return;
   }
-  const int a = offset(2 * pair), b = max(a, offset(2 * pair + 1)), e = max(b, offset(2 * pair + 2));
   const auto live = [&](int t) { return p.targets[t] >= 0 && p.targets[t] < p.V; };
-  double chosen = 0.0, rejected = 0.0;
-  for (int t = a + tid; t < e; t += LOSS_THREADS) {
-    const double x = live(t) ? (double)p.logp[t] - (p.ref_logp ? (double)p.ref_logp[t] : 0.0) : 0.0;
-    (t < b ? chosen : rejected) += x;
+  double total = 0.0;
+  for (int pair = ALL ? wave : blockIdx.x; pair < p.n_pairs; pair += ALL ? WAVES : p.n_pairs) {
+    const int a = offset(2 * pair), b = max(a, offset(2 * pair + 1)), e = max(b, offset(2 * pair + 2)), first = a + (ALL ? lane : tid);
+    double chosen = 0.0, rejected = 0.0;
+    for (int t = first; t < e; t += STEP) {
+      const float logp = p.logp[t], ref = p.ref_logp ? p.ref_logp[t] : 0.f;
+      const double x = live(t) ? (double)logp - (double)ref : 0.0;
+      (t < b ? chosen : rejected) += x;
+    }
+    chosen = wave_sum64(chosen);
+    rejected = wave_sum64(rejected);
+    if (!ALL) {
+      if (lane == 0) { shared[0][wave] = chosen; shared[1][wave] = rejected; }
+      __syncthreads();
+      chosen = wave_sum64(lane < WAVES ? shared[0][lane] : 0.0);
+      rejected = wave_sum64(lane < WAVES ? shared[1][lane] : 0.0);
+    }
+    const float m = (float)((double)p.beta * (chosen - rejected));
+    // -log sigma(m) = max(-m, 0) + log(1 + exp(-|m|))
+    const float tail = log1pf(expf(-fabsf(m)));
+    const float value = (1.f - p.smoothing) * (fmaxf(-m, 0.f) + tail) + p.smoothing * (fmaxf(m, 0.f) + tail);
+    if ((ALL ? lane : tid) == 0) p.pair_loss[pair] = value;
+    total += value;
+    const float dm = p.smoothing / (1.f + expf(-m)) - (1.f - p.smoothing) / (1.f + expf(m));
+    const float slope = p.scale * p.loss_scale * p.beta * dm;
+    for (int t = first; t < e; t += STEP) p.dlogp[t] = live(t) ? (t < b ? slope : -slope) : 0.f;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    chosen += __shfl_xor(chosen, o, 64);
-    rejected += __shfl_xor(rejected, o, 64);
-  }
-  if ((tid & 63) == 0) { shared[0][tid >> 6] = chosen; shared[1][tid >> 6] = rejected; }
+  if (!ALL || !loss) return;
+  if (lane == 0) shared[0][wave] = total;
   __syncthreads();
-  chosen = rejected = 0.0;
-#pragma unroll
-  for (int w = 0; w < LOSS_THREADS / 64; ++w) { chosen += shared[0][w]; rejected += shared[1][w]; }
-  const float m = (float)((double)p.beta * (chosen - rejected));
-  // -log sigma(m) = max(-m, 0) + log(1 + exp(-|m|))
-  const float tail = log1pf(expf(-fabsf(m)));
-  if (tid == 0) p.pair_loss[pair] = (1.f - p.smoothing) * (fmaxf(-m, 0.f) + tail) + p.smoothing * (fmaxf(m, 0.f) + tail);
-  const float dm = p.smoothing / (1.f + expf(-m)) - (1.f - p.smoothing) / (1.f + expf(m));
-  const float slope = p.scale * p.loss_scale * p.beta * dm;
-  for (int t = a + tid; t < e; t += LOSS_THREADS) p.dlogp[t] = live(t) ? (t < b ? slope : -slope) : 0.f;
+  if (wave == 0) {
+    total = wave_sum64(lane < WAVES ? shared[0][lane] : 0.0);
+    if (lane == 0) loss[0] = (float)(total * p.scale);
+  }
 }
 
-// The teacher's entries of a row; those without a token (an id outside the vocabulary) have id -1 and probability 0.
-struct DistillRow {
-  int id[kDistillMax];
-  float p[kDistillMax];
+// What the first wave, which takes the teacher's entries of a row, tells the others.
+struct DistillList {
+  int id[kDistillMax];                     // -1: no token
+  float p[kDistillMax], z[kDistillMax];    // the teacher's logit / temperature, then its probability; the student's logit
+  int any;                                 // a token is named at all
+  float mass;                              // sum of p
+  float top, sum;                          // of the named tokens' logits, each once: maximum; sum of exp((z - top) / temperature)
+  float gain;                              // sum of p (log p - (z - top) / temperature)
 };
-__global__ __launch_bounds__(LOSS_THREADS) void distill_loss_kernel(DistillArgs a) {
-  extern __shared__ uint32_t named[];                 // a bit per token of the vocabulary: the teacher has named it
-  __shared__ DistillRow list;
-  __shared__ float shared[LOSS_THREADS / 64];
-  const int64_t t = blockIdx.x;
-  const int tid = threadIdx.x, V = a.V, K = a.K;
-  const float w = a.weight[t], c = a.log2e_by_temperature, per = 1.f / a.temperature;
-  const elem_t* row = (const elem_t*)a.logits + t * a.ld;
-  elem_t* out = (elem_t*)a.dlogits + t * a.ld_d;
+// id, u: the lane's first entry, if it has one
+__device__ __forceinline__ void distill_list(const DistillArgs& a, int64_t t, const elem_t* row, uint32_t* named, DistillList& l, int lane, int id,
+                                             float u, int& twice) {
+  const int K = a.K;
+  const float c = a.log2e_by_temperature, per = 1.f / a.temperature;
   constexpr OpMax op_max;
   constexpr OpSum op_sum;
-  int any = 0, twice = 0;
-  float top = -INFINITY;
-  if (w != 0.f) {
-    for (int i = tid; i < (V + 31) / 32; i += LOSS_THREADS) named[i] = 0;
-    __syncthreads();
-    for (int j = tid; j < K; j += LOSS_THREADS) {
-      int id = a.ids[t * a.ld_teacher + j];
-      if (id < 0 || id >= V) id = -1;
-      list.id[j] = id;
-      if (id < 0) continue;
-      any = 1;
-      const uint32_t bit = 1u << (id & 31);
-      if (atomicOr(&named[id >> 5], bit) & bit) twice = 1;
-      top = fmaxf(top, a.teacher[t * a.ld_teacher + j]);
+  int any = 0;
+  twice = 0;
+  float top_u = -INFINITY, top = -INFINITY;
+  for (int j = lane; j < K; j += 64) {
+    if (j >= 64) {
+      id = a.ids[t * a.ld_teacher + j];
+      u = a.teacher[t * a.ld_teacher + j];
     }
-    any = __syncthreads_or(any);
-    twice = __syncthreads_or(twice);
+    if (id < 0 || id >= a.V) id = -1;
+    l.id[j] = id;
+    if (id < 0) continue;
+    any = 1;
+    const float z = (float)row[id];
+    const uint32_t bit = 1u << (id & 31);
+    if (atomicOr(&named[id >> 5], bit) & bit) twice = 1;
+    l.z[j] = z;
+    l.p[j] = u *= per;
+    top_u = fmaxf(top_u, u);
+    top = fmaxf(top, z);
   }
-  if (!any) {
-    if (tid == 0) a.token_loss[t] = 0.f;
-    if (a.dlogits) write_gradient(nullptr, out, V, 0, RowStats{0.f, 1.f}, 0.f, tid);
-    return;
-  }
+  any = __any(any);
+  twice = __any(twice);
+  if (lane == 0) l.any = any;
+  if (!any) return;
   // log p = (u - lse_u) of the teacher
   float lse_u;
   if (a.teacher_lse) {
     lse_u = a.teacher_lse[t];
   } else {
-    top = block_all<LOSS_THREADS>(top, shared, op_max);
+    top_u = wave_all(top_u, op_max);
     float sum = 0.f;
-    for (int j = tid; j < K; j += LOSS_THREADS)
-      if (list.id[j] >= 0) sum += exp_scaled(a.teacher[t * a.ld_teacher + j] - top, c);
-    lse_u = top * per + logf(block_all<LOSS_THREADS>(sum, shared, op_sum));
+    for (int j = lane; j < K; j += 64)
+      if (l.id[j] >= 0) sum += __builtin_amdgcn_exp2f((l.p[j] - top_u) * kLog2eLoss);
+    lse_u = top_u + logf(wave_all(sum, op_sum));
   }
-  float mass = 0.f;
-  for (int j = tid; j < K; j += LOSS_THREADS) {
-    const float p = list.id[j] >= 0 ? expf(a.teacher[t * a.ld_teacher + j] * per - lse_u) : 0.f;
-    list.p[j] = p;
+  top = wave_all(top, op_max);
+  const float from = top == -INFINITY ? 0.f : top;
+  float mass = 0.f, gain = 0.f, sum = 0.f;
+  for (int j = lane; j < K; j += 64) {
+    const int id = l.id[j];
+    if (id < 0) continue;
+    const float z = l.z[j], logp = l.p[j] - lse_u, p = expf(logp);
+    l.p[j] = p;
     mass += p;
-  }
-  // the student: the named tokens, each once, and all others
-  RowStats s{-INFINITY, 0.f}, r{-INFINITY, 0.f};
-  __syncthreads();
-  const auto first = [&](int j) {                     // of the entries with this token
-    if (list.id[j] < 0) return false;
+    if (p != 0.f) gain += p * (logp - (z - from) * per);
+    bool first = true;
     if (twice)
-      for (int i = 0; i < j; ++i)
-        if (list.id[i] == list.id[j]) return false;
-    return true;
-  };
-  for (int j = tid; j < K; j += LOSS_THREADS)
-    if (first(j)) {
-      elemx8 v;
-      v[0] = row[list.id[j]];
-      stats_add(s, v, 1, c);
-    }
-  for (int x = tid * 8; x < V; x += LOSS_THREADS * 8) {
-    elemx8 v = load_chunk(row + x, V - x);
-    const uint32_t bits = named[x >> 5] >> (x & 31) & 0xff;
-    if (bits) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (bits >> i & 1) v[i] = (elem_t)-INFINITY;
-    }
-    stats_add(r, v, V - x, c);
+      for (int i = 0; i < j; ++i) first &= l.id[i] != id;
+    if (first) sum += __builtin_amdgcn_exp2f((z - from) * c);
   }
-  s = stats_join<LOSS_THREADS>(s, c, shared);
-  r = stats_join<LOSS_THREADS>(r, c, shared);
-  const float m = fmaxf(s.m, r.m);
-  const float others = r.m == -INFINITY ? 0.f : exp_scaled(r.m - m, c), all = s.sum * exp_scaled(s.m - m, c) + r.sum * others;
+  mass = wave_all(mass, op_sum);
+  gain = wave_all(gain, op_sum);
+  sum = wave_all(sum, op_sum);
+  if (lane == 0) { l.mass = mass; l.gain = gain; l.sum = sum; l.top = from; }
+}
+
+template <int THREADS, int CHUNKS>
+__global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void distill_loss_kernel(DistillArgs a) {
+  extern __shared__ uint32_t named[];                 // a bit per token of the vocabulary: the teacher has named it
+  __shared__ DistillList list;
+  __shared__ RowShared<THREADS> shared;
+  const int64_t t = blockIdx.x;
+  const int tid = threadIdx.x, V = a.V, K = a.K;
+  const float w = a.weight[t], c = a.log2e_by_temperature, per = 1.f / a.temperature;
+  const elem_t* const logits = (const elem_t*)a.logits + t * a.ld;
+  elem_t* const out = (elem_t*)a.dlogits + t * a.ld_d;
+  if (w == 0.f) {
+    if (tid == 0) a.token_loss[t] = 0.f;
+    if (a.dlogits) store_zeros<THREADS>(out, V, tid);
+    return;
+  }
+  // the entries are on their way in front of the row
+  int id = -1, twice = 0;
+  float u = 0.f;
+  if (tid < 64 && tid < K) {
+    id = a.ids[t * a.ld_teacher + tid];
+    u = a.teacher[t * a.ld_teacher + tid];
+  }
+  Row<THREADS, CHUNKS> row;
+  row.load(logits, V, tid);
+  for (int i = tid; i < (V + 31) / 32; i += THREADS) named[i] = 0;
+  __syncthreads();
+  if (tid < 64) distill_list(a, t, logits, named, list, tid, id, u, twice);
+  __syncthreads();
+  if (!list.any) {
+    if (tid == 0) a.token_loss[t] = 0.f;
+    if (a.dlogits) store_zeros<THREADS>(out, V, tid);
+    return;
+  }
+  // the student's distribution: the tokens that are not named, and with them those that are
+  row.without((const uint8_t*)named, V, tid);
+  const RowStats r = row.stats(c, shared);
+  const float r_sum = r.sum * __builtin_amdgcn_exp2f(-r.e.low);
+  const float m = list.sum == 0.f ? r.e.m : r_sum > 0.f ? fmaxf(list.top, r.e.m) : list.top;
+  const float others = __builtin_amdgcn_exp2f((r.e.m - m) * c), all = list.sum * __builtin_amdgcn_exp2f((list.top - m) * c) + (r_sum > 0.f ? r_sum * others : r_sum);
   const float log_all = logf(all);
-  float loss = 0.f;
-  for (int j = tid; j < K; j += LOSS_THREADS)
-    if (list.p[j] != 0.f)
-      loss += list.p[j] * ((a.teacher[t * a.ld_teacher + j] * per - lse_u) - (((float)row[list.id[j]] - m) * per - log_all));
-  loss = block_all<LOSS_THREADS>(loss, shared, op_sum);
-  float rest = 0.f;
+  float loss = list.gain + list.mass * ((m - list.top) * per + log_all), rest = 0.f;
   if (a.teacher_lse) {
-    rest = 1.f - block_all<LOSS_THREADS>(mass, shared, op_sum);
+    rest = 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;
-    if (rest != 0.f) loss += rest * (logf(rest) - ((r.m - m) * per + logf(r.sum) - log_all));
+    if (rest != 0.f) loss += rest * (logf(rest) - ((r.e.m - m) * per + logf(r_sum) - log_all));
   }
   if (tid == 0) a.token_loss[t] = loss;
   if (!a.dlogits) return;
-  // q - p of the named tokens; of the others q (1 - P / Q), by the largest of them
-  const float g = w * a.loss_scale * per, f = r.sum != 0.f ? g * (others / all - rest / r.sum) : 0.f, rm = reference(r.m);
-  float mine[kDistillMax / LOSS_THREADS];
-#pragma unroll
-  for (int i = 0; i < kDistillMax / LOSS_THREADS; ++i) {
-    const int j = tid + i * LOSS_THREADS;
-    mine[i] = 0.f;
-    if (j >= K || !first(j)) continue;
-    float p = list.p[j];
-    if (twice)
-      for (int k = j + 1; k < K; ++k)
-        if (list.id[k] == list.id[j]) p += list.p[k];
-    mine[i] = g * (exp_scaled((float)row[list.id[j]] - m, c) / all - p);
-  }
-  __syncthreads();                                    // the row may be overwritten by its gradient
-  for (int x = tid * 8; x < V; x += LOSS_THREADS * 8) {
-    const elemx8 v = load_chunk(row + x, V - x);
-    elemx8 o;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = (elem_t)(exp_scaled((float)v[i] - rm, c) * f);
-    store_chunk(out + x, o, V - x);
-  }
+  // q - p of the named tokens; of the others q (1 - P / Q)
+  const float g = w * a.loss_scale * per;
+  const float f = r_sum == 0.f ? 0.f : g * (others / all - rest / r_sum) * __builtin_amdgcn_exp2f(-r.e.low);
+  row.store(out, V, tid, r.e, f);
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kDistillMax / LOSS_THREADS; ++i) {
-    const int j = tid + i * LOSS_THREADS;
-    if (j < K && first(j)) out[list.id[j]] = (elem_t)mine[i];
+  if (tid >= 64) return;
+  for (int j = tid; j < K; j += 64) {
+    const int id = list.id[j];
+    if (id < 0) continue;
+    float p = list.p[j];
+    bool first = true;
+    if (twice) {
+      for (int i = 0; i < j; ++i) first &= list.id[i] != id;
+      for (int i = j + 1; i < K; ++i)
+        if (list.id[i] == id) p += list.p[i];
+    }
+    if (first) out[id] = (elem_t)(g * (__builtin_amdgcn_exp2f((list.z[j] - m) * c) / all - p));
   }
 }
 
-// out[0] = scale * sum of x[i] * (weight ? weight[i] : 1): one workgroup, fixed order, 64-bit sums.
+// out[0] = scale * sum of x[i] * (weight ? weight[i] : 1): one workgroup, fixed order, 64-bit sums.  What a weight of 0 takes out is
+// finite: such tokens' losses are 0.
 __global__ __launch_bounds__(1024) void weighted_sum_kernel(int n, const float* __restrict__ x, const float* __restrict__ weight, float scale,
                                                             float* __restrict__ out) {
   __shared__ double shared[16];
   const int tid = threadIdx.x;
   double s = 0.0;
-  for (int i = tid; i < n; i += 1024) {
-    const float w = weight ? weight[i] : 1.f;
-    if (w != 0.f) s += (double)x[i] * w;
+  for (int i = tid; i < n; i += 8 * 1024) {
+    float v[8], w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int at = min(i + j * 1024, n - 1);
+      v[j] = x[at];
+      w[j] = weight ? weight[at] : 1.f;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i + j * 1024 < n) s += (double)v[j] * w[j];
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -336,29 +566,67 @@ static hipError_t launch_sum(int64_t n, const float* x, const float* weight, flo
   return hipGetLastError();
 }
 
+// Workgroups of 256 threads up to 8192 columns, 512 up to 16384 and 1024 above, with as many chunks per thread as a row has: up to 8, two
+// thousand threads on a CU; up to 16, half of them.  Above 131072 columns the row is read twice.  Policy loss, us, in GB/s of a read and a
+// written row: 8192 x 8200 with 512 threads 59 (4550), 1024 84; 8192 x 24576 512 155, 1024 147 (5480); 2048 x 131072 in registers 228
+// (4710), read twice 251.
+#define AXONN_ROW_CASE(KERNEL, THREADS, CHUNKS, LDS, ...)                                                                     \
+  case THREADS * 100 + CHUNKS: hipLaunchKernelGGL((KERNEL<THREADS, CHUNKS>), dim3((unsigned)T), dim3(THREADS), LDS, st, __VA_ARGS__); break
+#define AXONN_ROW_DISPATCH(KERNEL, LDS, ...)                                                                              \
+  switch (row_kernel(V)) {                                                                                                \
+    AXONN_ROW_CASE(KERNEL, 256, 1, LDS, __VA_ARGS__);  AXONN_ROW_CASE(KERNEL, 256, 2, LDS, __VA_ARGS__);                  \
+    AXONN_ROW_CASE(KERNEL, 256, 3, LDS, __VA_ARGS__);  AXONN_ROW_CASE(KERNEL, 256, 4, LDS, __VA_ARGS__);                  \
+    AXONN_ROW_CASE(KERNEL, 512, 3, LDS, __VA_ARGS__);  AXONN_ROW_CASE(KERNEL, 512, 4, LDS, __VA_ARGS__);                  \
+    AXONN_ROW_CASE(KERNEL, 1024, 3, LDS, __VA_ARGS__); AXONN_ROW_CASE(KERNEL, 1024, 4, LDS, __VA_ARGS__);                 \
+    AXONN_ROW_CASE(KERNEL, 1024, 5, LDS, __VA_ARGS__); AXONN_ROW_CASE(KERNEL, 1024, 6, LDS, __VA_ARGS__);                 \
+    AXONN_ROW_CASE(KERNEL, 1024, 7, LDS, __VA_ARGS__); AXONN_ROW_CASE(KERNEL, 1024, 8, LDS, __VA_ARGS__);                 \
+    AXONN_ROW_CASE(KERNEL, 1024, 10, LDS, __VA_ARGS__); AXONN_ROW_CASE(KERNEL, 1024, 12, LDS, __VA_ARGS__);               \
+    AXONN_ROW_CASE(KERNEL, 1024, 14, LDS, __VA_ARGS__); AXONN_ROW_CASE(KERNEL, 1024, 16, LDS, __VA_ARGS__);               \
+    default: hipLaunchKernelGGL((KERNEL<1024, 0>), dim3((unsigned)T), dim3(1024), LDS, st, __VA_ARGS__);                  \
+  }
+static int row_kernel(int64_t V) {
+  const int threads = V <= 8192 ? 256 : V <= 16384 ? 512 : 1024, chunks = (int)((V + 8 * threads - 1) / (8 * threads));
+  return chunks <= 8 ? threads * 100 + chunks : chunks <= 16 ? threads * 100 + (chunks + 1) / 2 * 2 : 0;
+}
+
 hipError_t launch_token_logprobs_fwd(int64_t T, int64_t V, const void* logits, int64_t ld, const int* targets, float* logp, float* lse,
                                      hipStream_t st) {
-  hipLaunchKernelGGL(token_logprobs_fwd_kernel, dim3((unsigned)T), dim3(LOSS_THREADS), 0, st, (int)V, (const elem_t*)logits, ld, targets,
-                     logp, lse);
+  AXONN_ROW_DISPATCH(token_logprobs_fwd_kernel, 0, (int)V, (const elem_t*)logits, ld, targets, logp, lse);
   return hipGetLastError();
 }
 hipError_t launch_token_logprobs_bwd(int64_t T, int64_t V, const void* logits, int64_t ld, const int* targets, const float* lse,
                                      const float* dlogp, void* dlogits, int64_t ld_d, hipStream_t st) {
-  hipLaunchKernelGGL(token_logprobs_bwd_kernel, dim3((unsigned)T), dim3(LOSS_THREADS), 0, st, (int)V, (const elem_t*)logits, ld, targets,
-                     lse, dlogp, (elem_t*)dlogits, ld_d);
+#define AXONN_GRADIENT(CHUNKS)                                                                                                  \
+  do {                                                                                                                     \
+    const uint32_t parts = (uint32_t)((V + 8 * GRAD_THREADS * CHUNKS - 1) / (8 * GRAD_THREADS * CHUNKS));                  \
+    hipLaunchKernelGGL(token_logprobs_bwd_kernel<CHUNKS>, dim3((unsigned)T * parts), dim3(GRAD_THREADS), 0, st, (int)V, parts,   \
+                       host::recip_of(parts), (const elem_t*)logits, ld, targets, lse, dlogp, (elem_t*)dlogits, ld_d);     \
+  } while (0)
+  // (a shorter kernel for short rows: 61 x 2000 2.6 us, 3.9 with the other one)
+  if (V <= 8 * GRAD_THREADS) AXONN_GRADIENT(1);
+  else AXONN_GRADIENT(4);
+#undef AXONN_GRADIENT
   return hipGetLastError();
 }
 hipError_t launch_policy_loss(int64_t T, const PolicyArgs& p, float* loss, hipStream_t st) {
-  hipLaunchKernelGGL(policy_loss_kernel, dim3((unsigned)T), dim3(LOSS_THREADS), 0, st, p);
+  const int64_t V = p.V;
+  AXONN_ROW_DISPATCH(policy_loss_kernel, 0, p);
   return launch_sum(T, p.token_loss, p.weight, 1.f, loss, st);
 }
 hipError_t launch_preference_loss(const PreferenceArgs& p, float* loss, hipStream_t st) {
-  hipLaunchKernelGGL(preference_loss_kernel, dim3((unsigned)p.n_pairs + 1), dim3(LOSS_THREADS), 0, st, p);
+  if (p.T <= PREF_ALONE) {
+    hipLaunchKernelGGL(preference_loss_kernel<true>, dim3(1), dim3(PREF_THREADS), 0, st, p, loss);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(preference_loss_kernel<false>, dim3((unsigned)p.n_pairs + 1), dim3(PREF_THREADS), 0, st, p, nullptr);
   return launch_sum(p.n_pairs, p.pair_loss, nullptr, p.scale, loss, st);
 }
 hipError_t launch_distill_loss(int64_t T, const DistillArgs& a, float* loss, hipStream_t st) {
-  hipLaunchKernelGGL(distill_loss_kernel, dim3((unsigned)T), dim3(LOSS_THREADS), (unsigned)((a.V + 31) / 32 * 4), st, a);
+  const int64_t V = a.V;
+  AXONN_ROW_DISPATCH(distill_loss_kernel, (unsigned)((V + 31) / 32 * 4), a);
   return launch_sum(T, a.token_loss, a.weight, 1.f, loss, st);
 }
+#undef AXONN_ROW_DISPATCH
+#undef AXONN_ROW_CASE
 
 }  // namespace axonn

@@ -174,8 +174,8 @@ int axonn_distill_loss(int64_t T, int64_t V, int32_t K, const void* logits, int6
   if (K > kDistillMax || V > kDistillMaxVocab)
     return fail_entry(AXONN_EUNSUPPORTED, "%s: at most %d entries per token and a vocabulary of %d", what, kDistillMax, kDistillMaxVocab);
   if (ld_teacher < K) return fail_entry(AXONN_EINVAL, "%s: ld_teacher < K", what);
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(1.f / temperature))
-    return fail_entry(AXONN_EINVAL, "%s: temperature must be positive and finite", what);
+  if (!(temperature >= 0x1p-16f && temperature <= 0x1p16f))
+    return fail_entry(AXONN_EINVAL, "%s: temperature must be in [2^-16, 2^16]", what);
   const DistillArgs a{(int)V, K, logits, ld_logits, teacher_logits, teacher_ids, ld_teacher, teacher_lse, weight, temperature,
                       (float)(1.4426950408889634 / temperature), loss_scale, token_loss, dlogits, ld_dlogits};
   LaunchTiming timing(PC_LOSSES, (hipStream_t)hip_stream);

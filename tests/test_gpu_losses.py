@@ -15,7 +15,7 @@ from test_gpu_step_ops import Padded, U, normal, within
 pytestmark = [pytest.mark.gpu, pytest.mark.parametrize("axonn_elem", ["bf16", "fp16"], indirect=True)]
 # rows, vocabulary, leading dimension, first element
 SIZES = [(1, 1, 1, 0), (3, 2, 5, 1), (4, 7, 7, 0), (5, 8, 8, 0), (6, 9, 12, 3), (3, 255, 255, 1), (9, 1000, 1000, 0), (4, 2047, 2050, 1), (4, 2049, 2049, 0),
-         (3, 4100, 4104, 8), (5, 8191, 8191, 0), (2, 16392, 16392, 0), (3, 32003, 32003, 1), (2, 51200, 51200, 0), (2, 70001, 70004, 1),
+         (3, 4100, 4104, 8), (5, 8191, 8191, 0), (2, 16392, 16392, 0), (3, 12289, 12289, 0), (3, 32003, 32003, 1), (2, 40968, 40968, 0), (2, 51200, 51200, 0), (2, 65536, 65536, 0), (2, 70001, 70004, 1), (1, 81921, 81921, 0), (1, 106497, 106497, 3), (1, 131071, 131071, 0),
          (2, 131080, 131080, 0), (1, 262144, 262144, 0), (1, 300007, 300007, 1)]
 
 
