@@ -605,7 +605,7 @@ int axonn_attention_packed_plan(int64_t T, int32_t n_seq, const int32_t* offsets
  * o [T, n_heads * head_dim]; lse [n_heads][T] float32.  Rows of o and lse that belong to no sequence are
  * left as they are, and nothing that lies in another row than a sequence's reaches its results.
  * head_dim a multiple of 4, at most 192; n_heads a multiple of n_kv_heads, at most 4096;
- * T * n_heads <= 2^27, n_seq * n_heads <= 2^23; leading dimensions at most 2^22; scale > 0
+ * T * n_heads <= 2^27, n_seq * n_heads <= 2^22; leading dimensions at most 2^22; scale > 0
  * (usually 1 / sqrt(head_dim)). */
 int axonn_attention_packed_fwd(int64_t T, int32_t n_seq, int32_t n_heads, int32_t n_kv_heads,
                                int32_t head_dim, float scale, const void* plan,

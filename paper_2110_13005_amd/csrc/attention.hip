@@ -96,7 +96,7 @@ __device__ __forceinline__ void dense_dkdv(DkdvLds<D>& lds, int id, int s, int a
   attn_bwd_dkdv<D, FITS>(lds, rank, s, d, rsqrtf((float)d), t.q, t.q + t.h, t.q + 2 * t.h, t.ld, dout + t.row * t.h + t.col, t.h,
                          lse + t.stat, delta + t.stat, dk, dk + t.h, t.ld);
 }
-template <int D, bool FITS, bool FORM_DELTA>
+template <int D, bool FITS, int FORM_DELTA>
 __device__ __forceinline__ void dense_dq(DqLds<D>& lds, int id, int s, int a, int n_bh, AttnWalk walk, int d,
                                          const elem_t* __restrict__ qkv, const elem_t* __restrict__ o,
                                          const elem_t* __restrict__ dout, const float* __restrict__ lse, float* delta,
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_bwd_dq_kernel(
     const elem_t* __restrict__ dout, const float* __restrict__ lse, float* __restrict__ delta,
     elem_t* __restrict__ dqkv, int by_4) {
   __shared__ DqLds<D> lds;
-  dense_dq<D, FITS, FORM_DELTA>(lds, blockIdx.x, s, a, n_bh, walk, d, qkv, o, dout, lse, delta, dqkv, by_4);
+  dense_dq<D, FITS, FORM_DELTA ? FORM_DELTA_EXACT : READ_DELTA>(lds, blockIdx.x, s, a, n_bh, walk, d, qkv, o, dout, lse, delta, dqkv, by_4);
 }
 // Both at once, for problems whose tiles do not fill the chip: the first half of the workgroups forms dK and dV, the second
 // dQ; delta is there already.  Each half alone is a chain of up to s / 128 (s / 64) tiles per workgroup on a part of the
@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256) void attn_bwd_both_kernel(
   __shared__ union { DkdvLds<D> dkdv; DqLds<D> dq; } lds;
   const int n = gridDim.x >> 1, id = blockIdx.x;
   if (id < n) dense_dkdv<D, FITS>(lds.dkdv, id, s, a, n_bh, walk, d, qkv, dout, lse, delta, dqkv);
-  else dense_dq<D, FITS, false>(lds.dq, id - n, s, a, n_bh, walk, d, qkv, nullptr, dout, lse, delta, dqkv, 0);
+  else dense_dq<D, FITS, READ_DELTA>(lds.dq, id - n, s, a, n_bh, walk, d, qkv, nullptr, dout, lse, delta, dqkv, 0);
 }
 
 // ------------------------------------------------------------------------- launchers

@@ -444,6 +444,13 @@ __device__ __forceinline__ float delta_add(float p, V ov, V dv, int first) {
 // ones of padded rows.  40 heads of 128 x 2048 125 -> 112 us, 16 of 128 x 8192 535 -> 477, 8 x 16 of 64 x 1024 60 -> 44 (two waves
 // per SIMD here, at 256 registers), against wait states in front of every MFMA, padded rows, tiles fetched into registers and
 // all of a block's exponentials beside 16 of its slots; 8 x 24 of 188 x 512 (block by block, tiles of 64) 119 -> 75.
+// Where partial sums of a tile lie: four columns of register quarter q of column tile dt, of dK (0) or dV (1), in a wave's 64 lanes.
+template <int D>
+__device__ __forceinline__ int partial_at(int wave, int which, int dt, int q, int lane) {
+  return (((wave * 2 + which) * (D / 32) + dt) * 4 + q) * 64 + lane;
+}
+template <int D>
+constexpr int partial_size() { return 4 * 2 * (D / 32) * 4 * 64; }         // of a tile of 128 keys, in floatx4
 template <int D>
 struct DkdvLds {
   static constexpr int BQ = D <= 128 ? 128 : 64, TILE = Tile<BQ, D>::BYTES, BUF = 2 * TILE, KEYS = Tile<128, D>::BYTES;
@@ -454,11 +461,12 @@ struct DkdvLds {
 };
 // GROUPED: the query tiles of `group` heads that share the keys, one head after the other, in the same pipeline: the next head's
 // first tile follows the last one of the head in front of it.  Their columns in q and dout lie d apart, their lse and delta stat_step.
+// With `partial` the sums (dK's without the scale) are left there in 32 bits, in the order of the registers (partial_at).
 template <int D, bool FITS, bool GROUPED = false>
 __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, int d, float scale, const elem_t* q, const elem_t* k,
                                               const elem_t* v, int64_t ld, const elem_t* dout, int64_t ld_do, const float* lse,
                                               const float* delta, elem_t* dk, elem_t* dv, int64_t ld_dkv, int group = 1,
-                                              int64_t stat_step = 0) {
+                                              int64_t stat_step = 0, floatx4* partial = nullptr) {
   static_assert(FITS || !GROUPED, "rows through registers are one head's");
   using L = DkdvLds<D>;
   constexpr int BQ = L::BQ, DT = D / 32, KK = D / 16;
@@ -527,7 +535,7 @@ __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, in
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) asm volatile("" : "+a"(dvacc[dt]), "+a"(dkacc[dt]));
 
-  constexpr int NB = BQ / 32, NS = 2 * KK, NG = 4 * DT, STEP = NS + NG, NSLOT = NB * STEP, W = 8;
+  constexpr int NB = BQ / 32, NS = 2 * KK, NG = 4 * DT, STEP = NS + NG, NSLOT = NB * STEP, W = GROUPED && D == 64 ? 4 : 8;
   static_assert(NB % 2 == 0 && NSLOT % W == 0 && NS % W == 0 && NG == NS, "block parity and ring position are the same in every tile");
   floatx16 sacc[2], pacc[2];            // scores and dP of two blocks: one being formed, one in its exponentials
   uint32_t pfw[2][8], dsw[2][8];        // P and dS of a block rounded to 16 bits, two per word: MFMA operands
@@ -687,6 +695,19 @@ __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, in
   for (int dt = 0; dt < DT; ++dt) mfma32_settle_agpr(dvacc[dt], dkacc[dt]);
   dma_wait_all();                 // copies of tiles beyond the last still write (zeros) to LDS
   __syncthreads();                // the tiles in LDS are done with
+  if constexpr (GROUPED) {
+    if (partial) {
+      if (kw0 >= s) return;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          partial[partial_at<D>(wave, 0, dt, j, lane)] = floatx4{dkacc[dt][4 * j], dkacc[dt][4 * j + 1], dkacc[dt][4 * j + 2], dkacc[dt][4 * j + 3]};
+          partial[partial_at<D>(wave, 1, dt, j, lane)] = floatx4{dvacc[dt][4 * j], dvacc[dt][4 * j + 1], dvacc[dt][4 * j + 2], dvacc[dt][4 * j + 3]};
+        }
+      return;
+    }
+  }
   constexpr int STAGED = 32 * (D + 8) * 2;
   static_assert(8 * STAGED <= sizeof(lds.tiles), "the result rows fit the tile buffers");
   store_rows_out<D, FITS>(lds.tiles + wave * STAGED, dkacc, scale, dk + (int64_t)kw0 * ld_dkv, ld_dkv, s - kw0, cols, lane);
@@ -697,7 +718,7 @@ __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, in
 // FORM_DELTA (d = D = 64 or 128): the kernel also forms delta (above) for its 128 queries, from the rows of dO and O, and
 // leaves it in `delta` for the dK / dV kernel, which then has to run behind this one: no launch of its own for it.  Else
 // `delta` is read and `o` ignored.  by_4: the sums in the order of the launch of its own, for sequences that take that launch
-// when they do not run with others.
+// when they do not run with others.  FORM_DELTA_ANY: for any d, in an order of its own.
 //
 // Two workgroups share a CU.  The fragments run a few MFMAs ahead through a ring, so that a wave waits for LDS only behind the
 // two barriers of a tile: one when everybody has left the tile before, whose buffer the memory pipeline then fills, one when
@@ -710,7 +731,8 @@ struct DqLds {
   __align__(1024) char tiles[2 * BUF];
   float delta[128];
 };
-template <int D, bool FITS, bool FORM_DELTA>
+enum FormDelta { READ_DELTA = 0, FORM_DELTA_EXACT = 1, FORM_DELTA_ANY = 2 };
+template <int D, bool FITS, int FORM_DELTA>
 __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d, float scale, const elem_t* q, const elem_t* k,
                                             const elem_t* v, int64_t ld, const elem_t* o, int64_t ld_o, const elem_t* dout,
                                             int64_t ld_do, const float* lse, float* delta, elem_t* dq, int64_t ld_dq, int by_4) {
@@ -732,7 +754,40 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
   elemx8 qf[KK], dof[KK];
   q_src.template fill<128>(buf0, q0);
   do_src.template fill<128>(buf1, q0);
-  if constexpr (FORM_DELTA) {
+  if constexpr (FORM_DELTA == FORM_DELTA_ANY) {
+    // a row's chunks in as many lanes as a power of two has; those behind the head's last column are zeros
+    constexpr int LPR = D == 192 ? 32 : D / 8, RSTEP = 256 / LPR, N = 128 / RSTEP, AT_ONCE = D == 192 ? 8 : N;
+    const int ch = tid % LPR;
+    const auto chunk = [&](const elem_t* row) {
+      union { elemx8 v; u32x4 w; u32x2 h[2]; } u;
+      u.w = u32x4{0, 0, 0, 0};
+      if (cols.has4(8 * ch + 4)) u.v = *reinterpret_cast<const elemx8*>(row + 8 * ch);
+      else if (cols.has4(8 * ch)) u.h[0] = *reinterpret_cast<const u32x2*>(row + 8 * ch);
+      return u.v;
+    };
+#pragma unroll
+    for (int j0 = 0; j0 < N; j0 += AT_ONCE) {
+      elemx8 ov[AT_ONCE], dv[AT_ONCE];
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        const int row = min(q0 + tid / LPR + (j0 + j) * RSTEP, s - 1);
+        ov[j] = chunk(o + (int64_t)row * ld_o);
+        dv[j] = chunk(dout + (int64_t)row * ld_do);
+      }
+#pragma unroll
+      for (int j = 0; j < AT_ONCE; ++j) {
+        float p = delta_add<8, false>(0.f, ov[j], dv[j], 0);
+#pragma unroll
+        for (int off = LPR / 2; off > 0; off >>= 1) p += __shfl_xor(p, off, 64);
+        const int row = tid / LPR + (j0 + j) * RSTEP;
+        if (ch == 0) {
+          lds.delta[row] = p;
+          if (q0 + row < s) delta[q0 + row] = p;
+        }
+      }
+    }
+  }
+  if constexpr (FORM_DELTA == FORM_DELTA_EXACT) {
     // O's rows and the same ones of dO: the D / 8 lanes that hold a row's chunks add up its products
     constexpr int LPR = D / 8, RSTEP = 256 / LPR, N = 128 / RSTEP;
     elemx8 ov[N], dv[N];
@@ -778,7 +833,7 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
   for (int kk = 0; kk < KK; ++kk) qf[kk] = frag_rows<128, D>(buf0, fl, wave, kk);
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) dof[kk] = frag_rows<128, D>(buf1, fl, wave, kk);
-  if constexpr (FORM_DELTA) delta_q = lds.delta[32 * wave + (lane & 31)];
+  if constexpr (FORM_DELTA != READ_DELTA) delta_q = lds.delta[32 * wave + (lane & 31)];
   else if (qi < s) delta_q = delta[qi];
   __syncthreads();                // the rows have been read
   k_src.template fill<BKV>(buf0, 0);

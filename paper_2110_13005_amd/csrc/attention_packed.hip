@@ -38,8 +38,65 @@ __device__ __forceinline__ int plan_scan(int v, int* shared, int tid, Op op, int
   return op(front, v);
 }
 
-// One workgroup.  Offsets that do not ascend or leave [0, T] are taken as the largest so far inside it.  The list's order among tiles
-// with the same work is left to the atomics: no result depends on it.
+// Offsets that do not ascend or leave [0, T] are taken as the largest so far inside it, in both kernels.
+//
+// Few sequences: every wave holds them all, a lane SEQS of them, and lists the tiles of one range of classes by itself: how many tiles
+// lie in the classes above is a sum over the sequences, a tile's place among its class a count of the lanes in front.  No barriers; 15
+// documents in 8192 rows in 2.9 us (by the other kernel 6.1).
+constexpr int PLAN_FEW = 256;
+template <int SEQS>
+__global__ __launch_bounds__(PLAN_THREADS) void attn_packed_plan_few_kernel(int T, int n_seq, const int* __restrict__ offsets,
+                                                                            PackedPlan* __restrict__ plan) {
+  constexpr int WAVES = PLAN_THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int start[SEQS], len[SEQS], tiles[SEQS];
+#pragma unroll
+  for (int i = 0; i < SEQS; ++i) {
+    const int at = 64 * i + lane;
+    start[i] = offsets[min(at, n_seq)];
+    len[i] = offsets[min(at + 1, n_seq)];
+  }
+  int upto = 0, most = 0, total = 0;
+#pragma unroll
+  for (int i = 0; i < SEQS; ++i) {
+    int top = min(max(start[i], 0), T);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(top, o, 64);
+      if (lane >= o) top = max(top, u);
+    }
+    start[i] = max(top, upto);
+    upto = __shfl(start[i], 63, 64);
+    len[i] = 64 * i + lane < n_seq ? max(min(max(len[i], 0), T) - start[i], 0) : 0;
+    tiles[i] = (len[i] + 127) / 128;
+    most = max(most, tiles[i]);
+    total += tiles[i];
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    most = max(most, __shfl_xor(most, o, 64));
+    total += __shfl_xor(total, o, 64);
+  }
+  if (threadIdx.x == 0) plan->n = total;
+  // this wave's classes, from the highest down
+  const int per = (most + WAVES - 1) / WAVES, high = most - wave * per, low = max(high - per, 0);
+  int place = 0;
+#pragma unroll
+  for (int i = 0; i < SEQS; ++i) place += max(tiles[i] - max(high, 0), 0);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) place += __shfl_xor(place, o, 64);
+  for (int c = high - 1; c >= low; --c) {
+#pragma unroll
+    for (int i = 0; i < SEQS; ++i) {
+      const unsigned long long mine = __ballot(tiles[i] > c);
+      if (tiles[i] > c) plan->items[place + __popcll(mine & ((1ull << lane) - 1))] = PlanItem{start[i], len[i], c, 0};
+      place += __popcll(mine);
+    }
+  }
+}
+
+// Any number: one workgroup sorts by counting.  The list's order among tiles with the same work is left to the atomics: no result
+// depends on it.
 __global__ __launch_bounds__(PLAN_THREADS) void attn_packed_plan_kernel(int T, int n_seq, const int* __restrict__ offsets,
                                                                         PackedPlan* __restrict__ plan) {
   __shared__ int at[PLAN_CLASSES];         // sequences by their number of tiles; then where each class's next tile goes in the list
@@ -135,6 +192,10 @@ struct PackedArgs {
   float* delta;
   elem_t* dqkv;
   int64_t ld_dqkv;
+  // dK / dV: workgroups that share a tile of keys, each with group / parts of its heads; above 1 they leave their sums in `partial`
+  int parts;
+  uint32_t units_recip, parts_recip;               // reciprocals of kv * parts and of parts
+  floatx4* partial;
 };
 
 struct PackedTile { int start, len, tile, unit; };
@@ -189,15 +250,54 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_packed_fwd_kernel(P
 template <int D>
 __device__ __forceinline__ void packed_dkdv(DkdvLds<D>& lds, const PackedArgs& p, uint32_t id) {
   PackedTile t;
-  if (!packed_tile(p, id, p.kv, p.kv_recip, t)) return;
-  const PackedHead h = packed_rows(p, t.start, t.unit * p.group, t.unit);
+  if (!packed_tile(p, id, p.kv * p.parts, p.units_recip, t)) return;
+  const int kv = host::recip_div(t.unit, p.parts, p.parts_recip), part = t.unit - kv * p.parts, heads = host::recip_div(p.group, p.parts, p.parts_recip);
+  const PackedHead h = packed_rows(p, t.start, kv * p.group + part * heads, kv);
   const int64_t stat = (int64_t)h.head * p.T + h.row;
-  elem_t* const dk = p.dqkv + h.row * p.ld_dqkv + (int64_t)(p.heads + h.kv) * p.d;
+  elem_t* const dk = p.dqkv + h.row * p.ld_dqkv + (int64_t)(p.heads + kv) * p.d;
   attn_bwd_dkdv<D, true, true>(lds, (t.len - 1) / 128 - t.tile, t.len, p.d, p.scale, h.q, h.k, h.v, p.ld,
                                p.dout + h.row * p.ld_do + (int64_t)h.head * p.d, p.ld_do, p.lse + stat, p.delta + stat, dk,
-                               dk + (int64_t)p.kv * p.d, p.ld_dqkv, p.group, p.T);
+                               dk + (int64_t)p.kv * p.d, p.ld_dqkv, heads, p.T,
+                               p.parts > 1 ? p.partial + (int64_t)id * partial_size<D>() : nullptr);
 }
-template <int D, bool FORM_DELTA>
+// The parts' sums: a workgroup per tile, key / value head, dK or dV and 32 columns; a lane has 32 columns' half of a row.
+template <int D>
+__global__ __launch_bounds__(256) void attn_packed_dkdv_join_kernel(PackedArgs p) {
+  constexpr int DT = D / 32, AT_ONCE = 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t id = blockIdx.x / (2 * DT), rest = blockIdx.x - id * (2 * DT), which = rest / DT, dt = rest - which * DT;
+  PackedTile t;
+  if (!packed_tile(p, id, p.kv, p.kv_recip, t)) return;
+  const int k = 128 * ((t.len - 1) / 128 - t.tile) + 32 * wave + (lane & 31);
+  if (k >= t.len) return;
+  const floatx4* const from = p.partial + (int64_t)id * p.parts * partial_size<D>() + partial_at<D>(wave, which, dt, 0, lane);
+  floatx4 acc[4] = {};
+  for (int first = 0; first < p.parts; first += AT_ONCE) {
+    floatx4 v[AT_ONCE][4];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = from[(int64_t)min(first + i, p.parts - 1) * partial_size<D>() + 64 * j];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] += first + i < p.parts ? v[i][j][e] : 0.f;
+  }
+  const float mul = which ? 1.f : p.scale;
+  elem_t* const out = p.dqkv + (t.start + (int64_t)k) * p.ld_dqkv + (int64_t)(p.heads + which * p.kv + t.unit) * p.d;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int col = 32 * dt + 8 * j + 4 * (lane >> 5);
+    if (col >= p.d) continue;
+    elemx4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = (elem_t)(acc[j][e] * mul);
+    *reinterpret_cast<elemx4*>(out + col) = v;
+  }
+}
+template <int D, int FORM_DELTA>
 __device__ __forceinline__ void packed_dq(DqLds<D>& lds, const PackedArgs& p, uint32_t id) {
   PackedTile t;
   if (!packed_tile(p, id, p.heads, p.heads_recip, t)) return;
@@ -213,40 +313,62 @@ __global__ __launch_bounds__(256) void attn_packed_bwd_dkdv_kernel(PackedArgs p)
   __shared__ DkdvLds<D> lds;
   packed_dkdv<D>(lds, p, blockIdx.x);
 }
-template <int D, bool FORM_DELTA>
+template <int D>
 __global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_packed_bwd_dq_kernel(PackedArgs p) {
   __shared__ DqLds<D> lds;
-  packed_dq<D, FORM_DELTA>(lds, p, blockIdx.x);
+  packed_dq<D, FORM_DELTA_ANY>(lds, p, blockIdx.x);
 }
 // Both at once, for problems whose tiles do not fill the chip: the first workgroups form dK and dV, the others dQ.
 template <int D>
 __global__ __launch_bounds__(256) void attn_packed_bwd_both_kernel(PackedArgs p, uint32_t n_dkdv) {
   __shared__ union { DkdvLds<D> dkdv; DqLds<D> dq; } lds;
   if (blockIdx.x < n_dkdv) packed_dkdv<D>(lds.dkdv, p, blockIdx.x);
-  else packed_dq<D, false>(lds.dq, p, blockIdx.x - n_dkdv);
+  else packed_dq<D, READ_DELTA>(lds.dq, p, blockIdx.x - n_dkdv);
 }
 
-// delta[head][row] = sum over the head's columns of dO o: 16 lanes per (row, head), 4 elements per lane and step.
+// delta[head][row] = sum over the head's columns of dO o, for the one-launch backward: LANES lanes per (row, head), 8 elements each,
+// DELTA_PAIRS pairs on their way at once.
+constexpr int DELTA_PAIRS = 4;
+template <int D>
 __global__ __launch_bounds__(256) void attn_packed_delta_kernel(PackedArgs p) {
-  const int64_t pair = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int j = threadIdx.x & 15;
-  const int64_t row = pair / p.heads;
-  const int head = (int)(pair - row * p.heads);
-  float sum = 0.f;
-  if (row < p.T) {
-    const elem_t* o = p.o + row * p.ld_o + (int64_t)head * p.d;
-    const elem_t* dout = p.dout + row * p.ld_do + (int64_t)head * p.d;
-    for (int c = 4 * j; c < p.d; c += 64)
-      sum = delta_add<4, true>(sum, *reinterpret_cast<const elemx4*>(o + c), *reinterpret_cast<const elemx4*>(dout + c), 0);
+  constexpr int LANES = D == 192 ? 32 : D / 8;
+  const int ch = threadIdx.x % LANES, n = p.d - 8 * ch;
+  const uint32_t group = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, pairs = (uint32_t)p.T * p.heads;      // at most 2^27
+  elemx8 o[DELTA_PAIRS], g[DELTA_PAIRS];
+  uint32_t row[DELTA_PAIRS], head[DELTA_PAIRS];
+  const auto chunk = [&](const elem_t* q) {
+    union { elemx8 v; u32x4 w; u32x2 h[2]; } u;
+    u.w = u32x4{0, 0, 0, 0};
+    if (n >= 8) u.v = *reinterpret_cast<const elemx8*>(q);
+    else if (n >= 4) u.h[0] = *reinterpret_cast<const u32x2*>(q);
+    return u.v;
+  };
+#pragma unroll
+  for (int i = 0; i < DELTA_PAIRS; ++i) {
+    const uint32_t pair = min(group * DELTA_PAIRS + i, pairs - 1);
+    row[i] = host::recip_div(pair, p.heads, p.heads_recip);
+    head[i] = pair - row[i] * p.heads;
+    const int64_t col = (int64_t)head[i] * p.d + 8 * ch;
+    o[i] = chunk(p.o + row[i] * p.ld_o + col);
+    g[i] = chunk(p.dout + row[i] * p.ld_do + col);
   }
 #pragma unroll
-  for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-  if (row < p.T && j == 0) p.delta[(int64_t)head * p.T + row] = sum;
+  for (int i = 0; i < DELTA_PAIRS; ++i) {
+    float sum = delta_add<8, false>(0.f, o[i], g[i], 0);
+#pragma unroll
+    for (int off = LANES / 2; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (ch == 0 && group * DELTA_PAIRS + i < pairs) p.delta[(int64_t)head[i] * p.T + row[i]] = sum;
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------- launchers
 hipError_t launch_attention_packed_plan(int64_t T, int64_t n_seq, const int* offsets, void* plan, hipStream_t st) {
-  hipLaunchKernelGGL(attn_packed_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, (int)T, (int)n_seq, offsets, (PackedPlan*)plan);
+  if (n_seq <= 64)
+    hipLaunchKernelGGL(attn_packed_plan_few_kernel<1>, dim3(1), dim3(PLAN_THREADS), 0, st, (int)T, (int)n_seq, offsets, (PackedPlan*)plan);
+  else if (n_seq <= PLAN_FEW)
+    hipLaunchKernelGGL(attn_packed_plan_few_kernel<PLAN_FEW / 64>, dim3(1), dim3(PLAN_THREADS), 0, st, (int)T, (int)n_seq, offsets, (PackedPlan*)plan);
+  else
+    hipLaunchKernelGGL(attn_packed_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, (int)T, (int)n_seq, offsets, (PackedPlan*)plan);
   return hipGetLastError();
 }
 
@@ -259,19 +381,31 @@ static PackedArgs packed_args(const PackedShape& s, const void* plan) {
   return p;
 }
 
+static int packed_columns(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 192; }
+static int packed_parts(const PackedShape& s) { return host::packed_parts(s.T, s.n_seq, s.heads, s.kv, packed_columns(s.d)); }
+static uint64_t delta_bytes(const PackedShape& s) { return ((uint64_t)s.T * (uint64_t)s.heads * 4 + 255) / 256 * 256; }
+uint64_t attention_packed_bwd_ws_bytes(const PackedShape& s) {
+  const int parts = packed_parts(s);
+  return delta_bytes(s) + (parts > 1 ? (uint64_t)packed_tiles_bound(s.T, s.n_seq) * s.kv * parts * 128 * 2 * packed_columns(s.d) * 4 : 0);
+}
+
+#define AXONN_PACKED(KERNEL, GRID, ...)                                                                     \
+  do {                                                                                                 \
+    if (s.d <= 64) hipLaunchKernelGGL(KERNEL<64>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);          \
+    else if (s.d <= 128) hipLaunchKernelGGL(KERNEL<128>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);   \
+    else hipLaunchKernelGGL(KERNEL<192>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);                   \
+    const hipError_t e = hipGetLastError();                                                            \
+    if (e != hipSuccess) return e;                                                                     \
+  } while (0)
+
 hipError_t launch_attention_packed_fwd(const PackedShape& s, const void* plan, const void* qkv, int64_t ld, void* o, int64_t ld_o, float* lse,
                                        hipStream_t st) {
   PackedArgs p = packed_args(s, plan);
   p.qkv = (const elem_t*)qkv; p.ld = ld;
   p.o = (elem_t*)o; p.ld_o = ld_o; p.lse = lse;
-  const dim3 grid((unsigned)(packed_tiles_bound(s.T, s.n_seq) * s.heads));
-  if (s.d <= 64) hipLaunchKernelGGL(attn_packed_fwd_kernel<64>, grid, dim3(256), 0, st, p);
-  else if (s.d <= 128) hipLaunchKernelGGL(attn_packed_fwd_kernel<128>, grid, dim3(256), 0, st, p);
-  else hipLaunchKernelGGL(attn_packed_fwd_kernel<192>, grid, dim3(256), 0, st, p);
-  return hipGetLastError();
+  AXONN_PACKED(attn_packed_fwd_kernel, (unsigned)(packed_tiles_bound(s.T, s.n_seq) * s.heads), p);
+  return hipSuccess;
 }
-
-uint64_t attention_packed_bwd_ws_bytes(const PackedShape& s) { return 4u * (uint64_t)s.T * (uint64_t)s.heads; }
 
 hipError_t launch_attention_packed_bwd(const PackedShape& s, const void* plan, const void* qkv, int64_t ld, const void* o, int64_t ld_o,
                                        const float* lse, const void* dout, int64_t ld_do, void* dqkv, int64_t ld_dqkv, void* workspace,
@@ -282,33 +416,22 @@ hipError_t launch_attention_packed_bwd(const PackedShape& s, const void* plan, c
   p.dout = (const elem_t*)dout; p.ld_do = ld_do;
   p.dqkv = (elem_t*)dqkv; p.ld_dqkv = ld_dqkv;
   p.delta = (float*)workspace;
+  p.parts = packed_parts(s);
+  p.parts_recip = host::recip_of(p.parts); p.units_recip = host::recip_of(p.kv * p.parts);
+  p.partial = (floatx4*)((char*)workspace + delta_bytes(s));
   const int64_t tiles = packed_tiles_bound(s.T, s.n_seq);
-  const unsigned n_dq = (unsigned)(tiles * s.heads), n_dkdv = (unsigned)(tiles * s.kv);
-  const bool both = n_dq <= 256;
-  if (both || (s.d != 64 && s.d != 128)) {
-    hipLaunchKernelGGL(attn_packed_delta_kernel, dim3((unsigned)((s.T * s.heads + 15) / 16)), dim3(256), 0, st, p);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  const unsigned n_dq = (unsigned)(tiles * s.heads), n_join = (unsigned)(tiles * s.kv), n_dkdv = n_join * p.parts;
+  if (host::packed_one_launch(n_dq, packed_columns(s.d))) {
+    const int per_block = 256 * DELTA_PAIRS / (s.d > 128 ? 32 : packed_columns(s.d) / 8);
+    AXONN_PACKED(attn_packed_delta_kernel, (unsigned)((s.T * s.heads + per_block - 1) / per_block), p);
+    AXONN_PACKED(attn_packed_bwd_both_kernel, n_dq + n_dkdv, p, n_dkdv);
+  } else {
+    AXONN_PACKED(attn_packed_bwd_dq_kernel, n_dq, p);       // forms delta
+    AXONN_PACKED(attn_packed_bwd_dkdv_kernel, n_dkdv, p);
   }
-  if (both) {
-    const dim3 grid(n_dq + n_dkdv);
-    if (s.d <= 64) hipLaunchKernelGGL(attn_packed_bwd_both_kernel<64>, grid, dim3(256), 0, st, p, n_dkdv);
-    else if (s.d <= 128) hipLaunchKernelGGL(attn_packed_bwd_both_kernel<128>, grid, dim3(256), 0, st, p, n_dkdv);
-    else hipLaunchKernelGGL(attn_packed_bwd_both_kernel<192>, grid, dim3(256), 0, st, p, n_dkdv);
-    return hipGetLastError();
-  }
-  // where the dQ kernel forms delta it has to be the first
-  if (s.d == 64) hipLaunchKernelGGL((attn_packed_bwd_dq_kernel<64, true>), dim3(n_dq), dim3(256), 0, st, p);
-  else if (s.d < 64) hipLaunchKernelGGL((attn_packed_bwd_dq_kernel<64, false>), dim3(n_dq), dim3(256), 0, st, p);
-  else if (s.d == 128) hipLaunchKernelGGL((attn_packed_bwd_dq_kernel<128, true>), dim3(n_dq), dim3(256), 0, st, p);
-  else if (s.d < 128) hipLaunchKernelGGL((attn_packed_bwd_dq_kernel<128, false>), dim3(n_dq), dim3(256), 0, st, p);
-  else hipLaunchKernelGGL((attn_packed_bwd_dq_kernel<192, false>), dim3(n_dq), dim3(256), 0, st, p);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (s.d <= 64) hipLaunchKernelGGL(attn_packed_bwd_dkdv_kernel<64>, dim3(n_dkdv), dim3(256), 0, st, p);
-  else if (s.d <= 128) hipLaunchKernelGGL(attn_packed_bwd_dkdv_kernel<128>, dim3(n_dkdv), dim3(256), 0, st, p);
-  else hipLaunchKernelGGL(attn_packed_bwd_dkdv_kernel<192>, dim3(n_dkdv), dim3(256), 0, st, p);
-  return hipGetLastError();
+  if (p.parts > 1) AXONN_PACKED(attn_packed_dkdv_join_kernel, n_join * (packed_columns(s.d) / 16), p);
+  return hipSuccess;
 }
+#undef AXONN_PACKED
 
 }  // namespace axonn

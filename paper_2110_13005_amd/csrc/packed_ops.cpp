@@ -26,8 +26,8 @@ int packed_shape(const char* what, int64_t T, int32_t n_seq, int32_t n_heads, in
   if (n_heads % n_kv_heads) return fail_entry(AXONN_EINVAL, "%s: n_heads must be a multiple of n_kv_heads", what);
   if (!(scale > 0.f) || !std::isfinite(scale)) return fail_entry(AXONN_EINVAL, "%s: scale must be positive and finite", what);
   if (head_dim % 4 || head_dim > 192) return fail_entry(AXONN_EUNSUPPORTED, "%s: head dim must be a multiple of 4, at most 192", what);
-  if (n_heads > 4096 || T * n_heads > (1 << 27) || (int64_t)n_seq * n_heads > (1 << 23))
-    return fail_entry(AXONN_EUNSUPPORTED, "%s: at most 4096 heads, 2^27 rows and 2^23 sequences times heads", what);
+  if (n_heads > 4096 || T * n_heads > (1 << 27) || (int64_t)n_seq * n_heads > (1 << 22))
+    return fail_entry(AXONN_EUNSUPPORTED, "%s: at most 4096 heads, 2^27 rows and 2^22 sequences times heads", what);
   s = PackedShape{T, n_seq, n_heads, n_kv_heads, head_dim, scale};
   return AXONN_OK;
 }

@@ -118,6 +118,9 @@ CASES = [
     # more tiles than the one-launch backward takes
     ([140] * 9 + [3], 16, 4, 128, 0, 5, 0, 0), ([140] * 9 + [300], 16, 16, 64, 0, 0, 0, 0), ([129] * 9, 16, 2, 188, 0, 0, 0, 0),
     ([131] * 9, 16, 8, 92, 0, 0, 2, 1), ([400, 300, 200, 100, 50, 20, 10, 1] * 2, 8, 1, 64, 0, 0, 0, 0), ([90] * 18, 24, 24, 40, 0, 0, 0, 0),
+    # tiles of keys shared out over workgroups, in one launch with dQ and in one of their own
+    ([600, 200], 16, 1, 64, 1, 1, 0, 0), ([500], 12, 1, 128, 0, 0, 0, 0), ([450, 90], 8, 1, 160, 0, 3, 4, 0), ([1000, 400, 290], 32, 1, 64, 0, 0, 0, 0),
+    ([900, 380, 130], 32, 2, 100, 0, 9, 0, 0),
 ]
 
 
@@ -189,12 +192,12 @@ def test_attention_rows_beyond_32_bit_offsets():
 
 @pytest.mark.parametrize("T,offsets", [
     (1, [0, 1]), (300, [0, 300]), (1000, [0, 0, 128, 256, 257, 1000, 1000]), (900, [5, 3, 400, 200, 901, 7]), (900, [-7, 20, 2000]),
-    (100000, "many"), (1 << 24, [0, 1 << 24]), (1 << 24, [0, 1 << 20, 1 << 23, (1 << 24) - 5]), (70, [70, 70])])
+    (100000, "many"), (5000, "200"), (70000, "256"), (70000, "257"), (1 << 24, [0, 1 << 24]), (1 << 24, [0, 1 << 20, 1 << 23, (1 << 24) - 5]), (70, [70, 70])])
 def test_plan(T, offsets):
     """Every tile of every sequence once, those with the most tiles in front of them first (as far as these are told apart)."""
     rng = np.random.default_rng(3)
-    if offsets == "many":
-        offsets = np.sort(rng.integers(0, T + 1, 5001))
+    if isinstance(offsets, str):
+        offsets = np.sort(rng.integers(0, T + 1, 1 + (5000 if offsets == "many" else int(offsets))))
     n = len(offsets) - 1
     plan = workspace(B.axonn_attention_packed_plan_bytes(T, n))
     B.axonn_attention_packed_plan(T, n, dev_i32(offsets), plan)

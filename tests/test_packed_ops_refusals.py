@@ -39,7 +39,7 @@ def shapes(fn, ok):
     each(UNS, fn, ok, {0: ((1 << 24) + 1,), 4: (62, 196, 256)})
     refused(UNS, fn, *with_args(ok, _2=4098))
     refused(UNS, fn, *with_args(ok, _0=(1 << 24) + 8 - 8, _2=16))             # 2^28 rows times heads
-    refused(UNS, fn, *with_args(ok, _1=1 << 20, _2=16))
+    refused(UNS, fn, *with_args(ok, _1=(1 << 19) + 1, _2=8))
 
 
 def test_attention_forward():
@@ -50,7 +50,7 @@ def test_attention_forward():
     each(INV, fn, ok, {8: (WIDTH - 1,), 10: (WIDTH_O - 1,), 6: (A + 4,), 11: (A + 2,), 9: (A,)})
     each(UNS, fn, ok, {8: ((1 << 22) + 1,), 10: ((1 << 22) + 1,)})
     text = comment_of("axonn_attention_packed_fwd")
-    for limit in ("head_dim a multiple of 4, at most 192", "at most 4096", "T * n_heads <= 2^27", "n_seq * n_heads <= 2^23",
+    for limit in ("head_dim a multiple of 4, at most 192", "at most 4096", "T * n_heads <= 2^27", "n_seq * n_heads <= 2^22",
                   "leading dimensions at most 2^22"):
         assert limit in text, limit
 
