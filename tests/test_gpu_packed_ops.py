@@ -8,7 +8,7 @@ import pytest
 
 from oracle import packed_ops as P
 from paper_2110_13005_amd import binding as B
-from helpers import dev_i32, host
+from helpers import dev_i32, host, rel_fro
 from test_gpu_step_ops import Padded, U, half_step, normal, within, workspace
 
 pytestmark = [pytest.mark.gpu, pytest.mark.parametrize("axonn_elem", ["bf16", "fp16"], indirect=True)]
@@ -275,3 +275,130 @@ def test_attention_on_two_streams_at_once():
     torch.cuda.synchronize()
     for a, w in zip(calls, want):
         assert all((x == y).all() for x, y in zip((a.o.t, a.lse, a.dqkv.t), w))
+
+
+@pytest.mark.parametrize("loss", ["policy", "prefer", "distill"])
+def test_a_training_step_on_packed_sequences(loss):
+    """Embedding, projection, query / key norms with positions inside the sequences, packed attention, residual, LayerNorm, head and loss,
+    and all of it backwards, against the same step written out in float64 with automatic differentiation."""
+    import torch
+    rng = np.random.default_rng(12)
+    lens, heads, kv, d, V, h = [40, 23, 0, 17, 1, 30], 8, 2, 32, 200, 256
+    off = np.concatenate([[0], np.cumsum(lens)])
+    T, n, width = 120, len(lens), (heads + 2 * kv) * d              # nine rows behind the last sequence
+    eps, scale, S = 1e-5, d ** -0.5, 64.0
+    inside = np.arange(T) < off[-1]
+    pos = np.concatenate([np.arange(m) for m in lens] + [np.zeros(T - off[-1], int)])
+    tokens = rng.integers(0, V, T)
+    targets = np.where(inside & (rng.random(T) < 0.8), rng.integers(0, V, T), -100)
+    W = dict(table=normal(rng, V, h, std=0.5), wqkv=normal(rng, h, width, std=h ** -0.5), gq=normal(rng, 1, d, std=0.1, mean=1.0)[0],
+             gk=normal(rng, 1, d, std=0.1, mean=1.0)[0], wo=normal(rng, heads * d, h, std=(heads * d) ** -0.5), lng=normal(rng, 1, h, std=0.1, mean=1.0)[0],
+             lnb=normal(rng, 1, h, std=0.1)[0], head=normal(rng, h, V, std=h ** -0.5))
+    inv_freq = 100.0 ** (-2.0 * np.arange(d // 2) / d)
+    old, ref = -5.3 + 0.3 * rng.standard_normal(T), -5.3 + 0.3 * rng.standard_normal(T)
+    A, weight = rng.standard_normal(T), np.where(targets >= 0, 1 / 64, 0.0)
+    K = 12
+    ids, teacher = np.stack([rng.choice(V, K, replace=False) for _ in range(T)]), rng.standard_normal((T, K))
+    teacher_lse = np.log(np.exp(teacher).sum(axis=1)) + 0.3
+
+    # the step in float64
+    P64 = {k: torch.tensor(np.asarray(v, np.float64), requires_grad=True) for k, v in W.items()}
+    x = P64["table"][torch.tensor(tokens)] * 2.0
+    qkv = (x @ P64["wqkv"]).view(T, heads + 2 * kv, d)
+    ang = torch.tensor(pos[:, None] * inv_freq)[:, None]
+
+    def rotated(z, gain):
+        z = gain * z / torch.sqrt((z * z).mean(dim=-1, keepdim=True) + eps)
+        a, b = z[..., :d // 2], z[..., d // 2:]
+        return torch.cat((a * torch.cos(ang) - b * torch.sin(ang), a * torch.sin(ang) + b * torch.cos(ang)), dim=-1)
+
+    q, k, v = rotated(qkv[:, :heads], P64["gq"]), rotated(qkv[:, heads:heads + kv], P64["gk"]), qkv[:, heads + kv:]
+    rows = []
+    for a, b in zip(off, off[1:]):
+        for i in range(heads if b > a else 0):
+            j = i // (heads // kv)
+            s = (scale * q[a:b, i] @ k[a:b, j].T).masked_fill(torch.ones(b - a, b - a, dtype=torch.bool).triu(1), -torch.inf)
+            rows.append((a, b, i, torch.softmax(s, dim=1) @ v[a:b, j]))
+    o = torch.zeros(T, heads, d, dtype=torch.float64)
+    for a, b, i, r in rows:
+        o[a:b, i] = r
+    y = o.view(T, -1) @ P64["wo"] + x
+    logits = torch.nn.functional.layer_norm(y, (h,), P64["lng"], P64["lnb"], eps) @ P64["head"]
+    logq = torch.log_softmax(logits, dim=1)
+    live = torch.tensor(targets >= 0)
+    logp = torch.where(live, logq[torch.arange(T), torch.tensor(np.maximum(targets, 0))], 0.0)
+    if loss == "policy":
+        r, x_ref = torch.exp(logp - torch.tensor(old)), torch.tensor(ref) - logp
+        each = -torch.minimum(r * torch.tensor(A), r.clamp(0.8, 1.2) * torch.tensor(A)) + 0.1 * (torch.exp(x_ref) - x_ref - 1)
+        total = (torch.where(live, each, 0.0) * torch.tensor(weight)).sum()
+    elif loss == "prefer":
+        gain = torch.where(live, logp - torch.tensor(ref), 0.0)
+        m = 0.5 * torch.stack([gain[off[2 * i]:off[2 * i + 1]].sum() - gain[off[2 * i + 1]:off[2 * i + 2]].sum() for i in range(n // 2)])
+        total = -torch.nn.functional.logsigmoid(m).sum() / (n // 2)
+    else:
+        lp = torch.tensor(teacher - teacher_lse[:, None])
+        rest, at = 1 - torch.exp(lp).sum(dim=1), torch.tensor(ids)
+        others = torch.logsumexp(logq.scatter(1, at, -torch.inf), dim=1)
+        each = (torch.exp(lp) * (lp - logq.gather(1, at))).sum(dim=1) + rest * (torch.log(rest) - others)
+        total = (each * torch.tensor(weight)).sum()
+    total.backward()
+
+    # the same on the GPU
+    dt = B.torch_elem_dtype()
+
+    def up(a, dtype=dt):
+        return torch.from_numpy(np.ascontiguousarray(a)).to(dtype).cuda()
+
+    def zeros(*shape, dtype=dt):
+        return torch.zeros(*shape, dtype=dtype, device="cuda")
+
+    f32 = torch.float32
+    G = {name: up(w) for name, w in W.items()}
+    offsets, tok, tgt = dev_i32(off), dev_i32(tokens), dev_i32(targets)
+    positions, freq = dev_i32(pos), up(inv_freq, torch.float64)
+    X, QKV, R, O, Y, N, Z = zeros(T, h), zeros(T, width), zeros(T, width), zeros(T, heads * d), zeros(T, h), zeros(T, h), zeros(T, V)
+    lse, stats = zeros(heads, T, dtype=f32), zeros(T, 2, dtype=f32)
+    plan = workspace(B.axonn_attention_packed_plan_bytes(T, n))
+    B.axonn_embedding_fwd(T, h, V, tok, G["table"], 2.0, X, h)
+    B.axonn_gemm_bf16(1, 0, B.EPI_BIAS, T, width, h, X, h, G["wqkv"], width, QKV, width)
+    norm = (T, T, heads, kv, d, d, 0)
+    B.axonn_qk_norm_rope_fwd(*norm, QKV, width, G["gq"], G["gk"], eps, positions, freq, R, width)
+    B.axonn_attention_packed_plan(T, n, offsets, plan)
+    shape = (T, n, heads, kv, d, scale, plan, R, width)
+    B.axonn_attention_packed_fwd(*shape, O, heads * d, lse)
+    B.axonn_gemm_bf16(1, 0, B.EPI_BIAS_RES, T, h, heads * d, O, heads * d, G["wo"], h, Y, h, res=X, ld_res=h)
+    B.axonn_layernorm_fwd(T, h, Y, G["lng"], G["lnb"], eps, N, stats)
+    B.axonn_gemm_bf16(1, 0, B.EPI_BIAS, T, V, h, N, h, G["head"], V, Z, V)
+    token_loss, out, lp_dev = zeros(T, dtype=f32), zeros(1, dtype=f32), zeros(T, dtype=f32)
+    w_dev = up(weight, f32)
+    if loss == "policy":
+        B.axonn_policy_loss(T, V, Z, V, tgt, up(old, f32), up(ref, f32), up(A, f32), w_dev, 0.2, 0.2, 0.1, S, lp_dev, token_loss, out, Z, V)
+    elif loss == "prefer":
+        lse_z, dlogp, pair = zeros(T, dtype=f32), zeros(T, dtype=f32), zeros(n // 2, dtype=f32)
+        B.axonn_token_logprobs_fwd(T, V, Z, V, tgt, lp_dev, lse_z)
+        B.axonn_preference_loss(T, n // 2, V, offsets, tgt, lp_dev, up(ref, f32), 0.5, 0.0, 1 / (n // 2), S, pair, out, dlogp)
+        B.axonn_token_logprobs_bwd(T, V, Z, V, tgt, lse_z, dlogp, Z, V)
+    else:
+        B.axonn_distill_loss(T, V, K, Z, V, up(teacher, f32), dev_i32(ids), K, up(teacher_lse, f32), 1.0, w_dev, S, token_loss, out, Z, V)
+    dN, dY, dO, dR, dX = zeros(T, h), zeros(T, h), zeros(T, heads * d), zeros(T, width), zeros(T, h)
+    grads = {name: zeros(*W[name].shape, dtype=f32) for name in ("head", "wo", "wqkv", "gq", "gk", "lng", "lnb", "table")}
+    B.axonn_gemm_bf16(0, 0, B.EPI_ACC_F32, h, V, T, N, h, Z, V, grads["head"], V)
+    B.axonn_gemm_bf16(1, 1, B.EPI_BIAS, T, h, V, Z, V, G["head"], V, dN, h)
+    B.axonn_layernorm_bwd(T, h, dN, Y, stats, G["lng"], None, dY, grads["lng"], grads["lnb"], zeros(2 * ((T + 63) // 64) * h, dtype=f32))
+    B.axonn_gemm_bf16(0, 0, B.EPI_ACC_F32, heads * d, h, T, O, heads * d, dY, h, grads["wo"], h)
+    B.axonn_gemm_bf16(1, 1, B.EPI_BIAS, T, heads * d, h, dY, h, G["wo"], h, dO, heads * d)
+    ws = workspace(B.axonn_attention_packed_bwd_workspace(T, n, heads, kv, d))
+    B.axonn_attention_packed_bwd(*shape, O, heads * d, lse, dO, heads * d, dR, width, ws)
+    ws = workspace(B.axonn_qk_norm_rope_bwd_workspace(T, heads, kv, d))
+    B.axonn_qk_norm_rope_bwd(*norm, dR, width, QKV, width, G["gq"], G["gk"], eps, positions, freq, dR, width, grads["gq"], grads["gk"], ws)
+    B.axonn_gemm_bf16(0, 0, B.EPI_ACC_F32, h, width, T, X, h, dR, width, grads["wqkv"], width)
+    B.axonn_gemm_bf16(1, 1, B.EPI_BIAS, T, h, width, dR, width, G["wqkv"], width, dX, h)
+    dX += dY
+    ws = workspace(B.axonn_embedding_bwd_workspace(T, h, V))
+    B.axonn_embedding_bwd(T, h, V, tok, dX, h, 2.0, grads["table"], 1, 0, ws)
+    # the bounds of the framework's own layers: outputs 2e-2, gradients 3e-2
+    assert rel_fro(host(O)[inside], o.detach().view(T, -1).numpy()[inside]) <= 2e-2
+    assert abs(host(out)[0] - total.item()) <= 2e-2 * abs(total.item()) + 1e-3
+    for name, g in grads.items():
+        want = P64[name].grad.numpy()
+        assert rel_fro(host(g) / S, want) <= 3e-2, (name, rel_fro(host(g) / S, want))
