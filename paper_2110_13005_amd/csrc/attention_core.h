@@ -240,23 +240,23 @@ __device__ __forceinline__ void store_rows_out(char* lds, const floatx16* acc, f
 // Against tiles fetched into registers, stored between two barriers, and each tile's fragments read in one go, us: 40 heads of
 // 128 x 2048 58.0 -> 52.0, 16 of 128 x 8192 311 -> 278 (990 TFLOP/s), 8 x 16 of 64 x 1024 28.4 -> 27.1, 8 x 24 of 188 x 512 (every
 // lane on a row of its own, 8 bytes at a time) 76 -> 50.6, 2 x 36 of 176 x 2048 256 -> 153.
-template <int D>
+template <int D, int KEYS = 64>
 struct FwdLds {
-  static constexpr int BKV = 64, BUF = 2 * Tile<BKV, D>::BYTES;
+  static constexpr int BKV = KEYS, BUF = 2 * Tile<BKV, D>::BYTES;
   // K and V tile, two of each, and at the end the O rows.  The Q rows lie in the second pair's place first; at D = 64 LDS has room
   // for one of their own, and the second pair is on its way from the start (8 heads of 1016 rows 15.3 -> 15.0 us).
   static constexpr bool OWN_Q = D == 64;
   static constexpr int Q_AT = OWN_Q ? 2 * BUF : BUF;
   __align__(1024) char tiles[Q_AT + Tile<128, D>::BYTES];
 };
-template <int D, bool FITS>
-__device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int d, float scale, const elem_t* q, const elem_t* k,
+template <int D, bool FITS, int KEYS = 64>
+__device__ __forceinline__ void attn_fwd_tile(FwdLds<D, KEYS>& lds, int qt, int s, int d, float scale, const elem_t* q, const elem_t* k,
                                               const elem_t* v, int64_t ld, elem_t* o, int64_t ld_o, float* lse) {
-  using L = FwdLds<D>;
-  constexpr int BKV = L::BKV, DT = D / 32, KK = D / 16, BUF = L::BUF, Q_AT = L::Q_AT;
+  using L = FwdLds<D, KEYS>;
+  constexpr int BKV = L::BKV, HALVES = BKV / 32, DT = D / 32, KK = D / 16, BUF = L::BUF, Q_AT = L::Q_AT;
   constexpr int STAGED = 128 * (D + 8) * 2;
   constexpr bool OWN_Q = L::OWN_Q;
-  static_assert(Tile<128, D>::BYTES == BUF && STAGED <= Q_AT + BUF, "rows staged in the tile buffers");
+  static_assert(Tile<128, D>::BYTES >= BUF && STAGED <= sizeof(lds.tiles), "rows staged in the tile buffers");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 5;
   const int q0 = qt * 128, qw0 = q0 + 32 * wave, qi = qw0 + (lane & 31);
   const float scale_log2 = kLog2e * scale;
@@ -297,11 +297,12 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
   // the wave's own: a last tile with every key in its future is left out (0 x Inf and 0 x NaN are not 0)
   const int n_own = min(n_kt, (qw0 + 31) / BKV + 1);
   // Fragments of a tile in the order of the MFMAs that take them: K's alternate between the tile's two 32-key halves.
-  auto k_frag = [&](LdsBytes buf, int i) { return frag_rows<BKV, D>(buf, fl, i & 1, i >> 1); };
+  auto k_frag = [&](LdsBytes buf, int i) { return frag_rows<BKV, D>(buf, fl, i % HALVES, i / HALVES); };
   auto v_frag = [&](LdsBytes buf, int i) { return frag_cols<BKV, D>(buf + Tile<BKV, D>::BYTES, fl, i / DT, i % DT); };
-  constexpr int NF = 2 * KK;                     // fragments of a K tile, and of a V tile
-  static_assert(NF == 4 * DT, "one V fragment per score MFMA and one K fragment per P V MFMA");
-  constexpr int EARLY = D == 128 ? 12 : NF;      // the other V fragments find registers when the scores have left theirs
+  constexpr int NF = HALVES * KK;                // fragments of a K tile, and of a V tile
+  static_assert(NF == 2 * HALVES * DT, "one V fragment per score MFMA and one K fragment per P V MFMA");
+  // the other V fragments find registers when the scores have left theirs
+  constexpr int EARLY = HALVES == 1 ? NF / 2 : D == 128 ? 12 : NF;
   elemx8 kfr[NF], vfr[NF];
 #pragma unroll
   for (int i = 0; i < NF; ++i) kfr[i] = k_frag(buf0, i);
@@ -312,15 +313,15 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
   for (int kt = 0; kt < n_own; ++kt) {
     const int k0 = kt * BKV;
     const LdsBytes buf = buf0 + (kt & 1) * BUF, next = buf0 + (~kt & 1) * BUF;
-    floatx16 sacc[2];
+    floatx16 sacc[HALVES];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < HALVES; ++ks)
 #pragma unroll
       for (int r = 0; r < 16; ++r) sacc[ks][r] = 0.f;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < NF; ++i) {
-      sacc[i & 1] = mfma32(kfr[i], qf[i >> 1], sacc[i & 1]);
+      sacc[i % HALVES] = mfma32(kfr[i], qf[i / HALVES], sacc[i % HALVES]);
       if (i < EARLY) vfr[i] = v_frag(buf, i);
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -330,7 +331,7 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
       asm volatile("" ::: "memory");            // keeps the compiler from turning the branch into selects
       const int last = qi - k0 - 4 * g;         // the lane's last key, counted from its first one
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < HALVES; ++ks)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           if (32 * ks + 8 * (r >> 2) + (r & 3) > last) sacc[ks][r] = -INFINITY;
@@ -339,7 +340,7 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
     // Row maximum of the raw scores; in units of the exponent (log2) it is mx * scale_log2 (the scale is positive).
     float mx = sacc[0][0];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < HALVES; ++ks)
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sacc[ks][r]);
     mx = max_with_other_half(mx) * scale_log2;
@@ -359,7 +360,7 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
     const float neg_m = -m_run;
     float psum = 0.f;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < HALVES; ++ks)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const float p = fast_exp2(fmaf(sacc[ks][r], scale_log2, neg_m));
@@ -367,9 +368,9 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
         psum += p;
       }
     l_run += psum;
-    elemx8 pf[4];
+    elemx8 pf[2 * HALVES];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) pf[c] = pack8(sacc[c >> 1], 8 * (c & 1));
+    for (int c = 0; c < 2 * HALVES; ++c) pf[c] = pack8(sacc[c >> 1], 8 * (c & 1));
 #pragma unroll
     for (int i = EARLY; i < NF; ++i) vfr[i] = v_frag(buf, i);
     // The next tile is in LDS, and everybody has taken this one's fragments: its buffer is filled with the tile after next
@@ -396,7 +397,22 @@ __device__ __forceinline__ void attn_fwd_tile(FwdLds<D>& lds, int qt, int s, int
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  if (n_own < n_kt) __syncthreads();
+  if (HALVES == 2) {
+    if (n_own < n_kt) __syncthreads();           // the tile that it has left out has a barrier
+  } else {
+    // up to three tiles that it has left out: their barriers, and its share of the tiles behind them
+    for (int kt = n_own; kt < n_kt; ++kt) {
+      if (kt + 1 < n_kt) {
+        dma_wait_all();
+        k_src.template clear_foreign<BKV>(buf0 + (~kt & 1) * BUF);
+      }
+      __syncthreads();
+      if (kt + 2 < n_kt) {
+        k_src.template fill<BKV>(buf0 + (kt & 1) * BUF, (kt + 2) * BKV);
+        v_src.template fill<BKV>(buf0 + (kt & 1) * BUF + Tile<BKV, D>::BYTES, (kt + 2) * BKV);
+      }
+    }
+  }
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
   dma_wait_all();                 // copies of tiles beyond the last still write (zeros) to LDS
   __syncthreads();                // the tiles in LDS are done with

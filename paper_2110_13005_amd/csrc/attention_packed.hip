@@ -198,15 +198,20 @@ struct PackedArgs {
   floatx4* partial;
 };
 
-struct PackedTile { int start, len, tile, unit; };
-// Workgroup id -> item of the plan and unit (head) of it; false: there is no such tile.  A list that is not a plan of these rows makes
-// no workgroup leave them.
-__device__ __forceinline__ bool packed_tile(const PackedArgs& p, uint32_t id, uint32_t units, uint32_t recip, PackedTile& t) {
+// A workgroup's item of the plan, on its way, and the unit (head) of it that the workgroup takes.  Grids have as many workgroups as a plan
+// has places, so that the item can be read beside the number of items.
+struct PackedTile {
+  int start, len, tile, unit, item, n;
+  // Is there such a tile?  A list that is not a plan of these rows makes no workgroup leave them.
+  __device__ __forceinline__ bool exists(int T) const {
+    return (item < n) & (len > 0) & (len <= T) & ((uint32_t)start <= (uint32_t)(T - len)) & ((uint32_t)tile <= (uint32_t)(len - 1) / 128u);
+  }
+};
+__device__ __forceinline__ PackedTile packed_tile(const PackedArgs& p, uint32_t id, uint32_t units, uint32_t recip) {
   const uint32_t i = host::recip_div(id, units, recip);
-  if ((int)i >= p.plan->n) return false;
-  const PlanItem it = p.plan->items[i];
-  t = PackedTile{it.start, it.len, it.tile, (int)(id - i * units)};
-  return it.start >= 0 && it.len > 0 && it.len <= p.T && it.start <= p.T - it.len && it.tile >= 0 && it.tile <= (it.len - 1) / 128;
+  const int n = p.plan->n;
+  const int4 it = *reinterpret_cast<const int4*>(&p.plan->items[i]);
+  return PackedTile{it.x, it.y, it.z, (int)(id - i * units), (int)i, n};
 }
 // Workgroups are dealt round-robin to the 8 XCDs, each with an L2 of its own: the heads that share keys and values go to as few of
 // them as there are heads for (a plan's item has `heads` workgroups, so the XCD is the unit modulo 8 if 8 divides them).
@@ -237,21 +242,22 @@ __device__ __forceinline__ PackedHead packed_rows(const PackedArgs& p, int start
 }
 
 template <int D>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_packed_fwd_kernel(PackedArgs p) {
-  __shared__ FwdLds<D> lds;
-  PackedTile t;
-  if (!packed_tile(p, blockIdx.x, p.heads, p.heads_recip, t)) return;
-  const int head = packed_head(p, t.unit);
-  const PackedHead h = packed_rows(p, t.start, head, host::recip_div(head, p.group, p.group_recip));
-  attn_fwd_tile<D, true>(lds, t.tile, t.len, p.d, p.scale, h.q, h.k, h.v, p.ld, p.o + h.row * p.ld_o + (int64_t)head * p.d, p.ld_o,
+__global__ __launch_bounds__(256, 2) void attn_packed_fwd_kernel(PackedArgs p) {
+  constexpr int KEYS = D > 128 ? 32 : 64;
+  __shared__ FwdLds<D, KEYS> lds;
+  const PackedTile t = packed_tile(p, blockIdx.x, p.heads, p.heads_recip);
+  const int head = packed_head(p, t.unit), kv = host::recip_div(head, p.group, p.group_recip);
+  if (!t.exists(p.T)) return;
+  const PackedHead h = packed_rows(p, t.start, head, kv);
+  attn_fwd_tile<D, true, KEYS>(lds, t.tile, t.len, p.d, p.scale, h.q, h.k, h.v, p.ld, p.o + h.row * p.ld_o + (int64_t)head * p.d, p.ld_o,
                          p.lse + (int64_t)head * p.T + h.row);
 }
 
 template <int D>
 __device__ __forceinline__ void packed_dkdv(DkdvLds<D>& lds, const PackedArgs& p, uint32_t id) {
-  PackedTile t;
-  if (!packed_tile(p, id, p.kv * p.parts, p.units_recip, t)) return;
+  const PackedTile t = packed_tile(p, id, p.kv * p.parts, p.units_recip);
   const int kv = host::recip_div(t.unit, p.parts, p.parts_recip), part = t.unit - kv * p.parts, heads = host::recip_div(p.group, p.parts, p.parts_recip);
+  if (!t.exists(p.T)) return;
   const PackedHead h = packed_rows(p, t.start, kv * p.group + part * heads, kv);
   const int64_t stat = (int64_t)h.head * p.T + h.row;
   elem_t* const dk = p.dqkv + h.row * p.ld_dqkv + (int64_t)(p.heads + kv) * p.d;
@@ -266,8 +272,8 @@ __global__ __launch_bounds__(256) void attn_packed_dkdv_join_kernel(PackedArgs p
   constexpr int DT = D / 32, AT_ONCE = 4;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t id = blockIdx.x / (2 * DT), rest = blockIdx.x - id * (2 * DT), which = rest / DT, dt = rest - which * DT;
-  PackedTile t;
-  if (!packed_tile(p, id, p.kv, p.kv_recip, t)) return;
+  const PackedTile t = packed_tile(p, id, p.kv, p.kv_recip);
+  if (!t.exists(p.T)) return;
   const int k = 128 * ((t.len - 1) / 128 - t.tile) + 32 * wave + (lane & 31);
   if (k >= t.len) return;
   const floatx4* const from = p.partial + (int64_t)id * p.parts * partial_size<D>() + partial_at<D>(wave, which, dt, 0, lane);
@@ -299,10 +305,10 @@ __global__ __launch_bounds__(256) void attn_packed_dkdv_join_kernel(PackedArgs p
 }
 template <int D, int FORM_DELTA>
 __device__ __forceinline__ void packed_dq(DqLds<D>& lds, const PackedArgs& p, uint32_t id) {
-  PackedTile t;
-  if (!packed_tile(p, id, p.heads, p.heads_recip, t)) return;
-  const int head = packed_head(p, t.unit);
-  const PackedHead h = packed_rows(p, t.start, head, host::recip_div(head, p.group, p.group_recip));
+  const PackedTile t = packed_tile(p, id, p.heads, p.heads_recip);
+  const int head = packed_head(p, t.unit), kv = host::recip_div(head, p.group, p.group_recip);
+  if (!t.exists(p.T)) return;
+  const PackedHead h = packed_rows(p, t.start, head, kv);
   const int64_t stat = (int64_t)head * p.T + h.row, col = (int64_t)head * p.d;
   attn_bwd_dq<D, true, FORM_DELTA>(lds, t.tile, t.len, p.d, p.scale, h.q, h.k, h.v, p.ld, p.o + h.row * p.ld_o + col, p.ld_o,
                                    p.dout + h.row * p.ld_do + col, p.ld_do, p.lse + stat, p.delta + stat,
