@@ -735,6 +735,9 @@ __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, in
 // leaves it in `delta` for the dK / dV kernel, which then has to run behind this one: no launch of its own for it.  Else
 // `delta` is read and `o` ignored.  by_4: the sums in the order of the launch of its own, for sequences that take that launch
 // when they do not run with others.  FORM_DELTA_ANY: for any d, in an order of its own.
+// PINNED: the accumulators in the accumulation registers, scores and all operands in ordinary ones, by assembly (see mfma32_agpr); for
+// a wave that is alone on its SIMD.  The compiler, which gives every MFMA of such a kernel accumulation registers, moves a quarter of what the
+// loop issues between the two kinds otherwise.
 //
 // Two workgroups share a CU.  The fragments run a few MFMAs ahead through a ring, so that a wave waits for LDS only behind the
 // two barriers of a tile: one when everybody has left the tile before, whose buffer the memory pipeline then fills, one when
@@ -748,7 +751,7 @@ struct DqLds {
   float delta[128];
 };
 enum FormDelta { READ_DELTA = 0, FORM_DELTA_EXACT = 1, FORM_DELTA_ANY = 2 };
-template <int D, bool FITS, int FORM_DELTA>
+template <int D, bool FITS, int FORM_DELTA, bool PINNED = false>
 __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d, float scale, const elem_t* q, const elem_t* k,
                                             const elem_t* v, int64_t ld, const elem_t* o, int64_t ld_o, const elem_t* dout,
                                             int64_t ld_do, const float* lse, float* delta, elem_t* dq, int64_t ld_dq, int by_4) {
@@ -771,8 +774,9 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
   q_src.template fill<128>(buf0, q0);
   do_src.template fill<128>(buf1, q0);
   if constexpr (FORM_DELTA == FORM_DELTA_ANY) {
-    // a row's chunks in as many lanes as a power of two has; those behind the head's last column are zeros
-    constexpr int LPR = D == 192 ? 32 : D / 8, RSTEP = 256 / LPR, N = 128 / RSTEP, AT_ONCE = D == 192 ? 8 : N;
+    // chunks behind the head's last column are zeros
+    static_assert(D <= 128, "a power of two of chunks per row");
+    constexpr int LPR = D / 8, RSTEP = 256 / LPR, N = 128 / RSTEP;
     const int ch = tid % LPR;
     const auto chunk = [&](const elem_t* row) {
       union { elemx8 v; u32x4 w; u32x2 h[2]; } u;
@@ -781,25 +785,22 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
       else if (cols.has4(8 * ch)) u.h[0] = *reinterpret_cast<const u32x2*>(row + 8 * ch);
       return u.v;
     };
+    elemx8 ov[N], dv[N];
 #pragma unroll
-    for (int j0 = 0; j0 < N; j0 += AT_ONCE) {
-      elemx8 ov[AT_ONCE], dv[AT_ONCE];
+    for (int j = 0; j < N; ++j) {
+      const int row = min(q0 + tid / LPR + j * RSTEP, s - 1);
+      ov[j] = chunk(o + (int64_t)row * ld_o);
+      dv[j] = chunk(dout + (int64_t)row * ld_do);
+    }
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) {
-        const int row = min(q0 + tid / LPR + (j0 + j) * RSTEP, s - 1);
-        ov[j] = chunk(o + (int64_t)row * ld_o);
-        dv[j] = chunk(dout + (int64_t)row * ld_do);
-      }
+    for (int j = 0; j < N; ++j) {
+      float p = delta_add<8, false>(0.f, ov[j], dv[j], 0);
 #pragma unroll
-      for (int j = 0; j < AT_ONCE; ++j) {
-        float p = delta_add<8, false>(0.f, ov[j], dv[j], 0);
-#pragma unroll
-        for (int off = LPR / 2; off > 0; off >>= 1) p += __shfl_xor(p, off, 64);
-        const int row = tid / LPR + (j0 + j) * RSTEP;
-        if (ch == 0) {
-          lds.delta[row] = p;
-          if (q0 + row < s) delta[q0 + row] = p;
-        }
+      for (int off = LPR / 2; off > 0; off >>= 1) p += __shfl_xor(p, off, 64);
+      const int row = tid / LPR + j * RSTEP;
+      if (ch == 0) {
+        lds.delta[row] = p;
+        if (q0 + row < s) delta[q0 + row] = p;
       }
     }
   }
@@ -859,6 +860,10 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dqacc[dt][r] = 0.f;
+  if constexpr (PINNED) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) asm volatile("" : "+a"(dqacc[dt]));
+  }
 
   const int n_kt = (kv_end + BKV - 1) / BKV;
   // the wave's own: a last tile with every key in its future is left out (0 x Inf and 0 x NaN are not 0)
@@ -890,17 +895,28 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       floatx16 sacc, pacc;
+      if constexpr (!PINNED) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
+        for (int r = 0; r < 16; ++r) sacc[r] = pacc[r] = 0.f;
+      }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
         const int j = ks * HALF + i;
-        if (i & 1) pacc = mfma32(ring[j % W], dof[i >> 1], pacc);
-        else sacc = mfma32(ring[j % W], qf[i >> 1], sacc);
+        if constexpr (PINNED) {
+          floatx16& acc = i & 1 ? pacc : sacc;
+          const elemx8& f = i & 1 ? dof[i >> 1] : qf[i >> 1];
+          if (i < 2) mfma32_vgpr_zero<false>(acc, ring[j % W], f);
+          else mfma32_vgpr<false>(acc, ring[j % W], f);
+        } else if (i & 1) {
+          pacc = mfma32(ring[j % W], dof[i >> 1], pacc);
+        } else {
+          sacc = mfma32(ring[j % W], qf[i >> 1], sacc);
+        }
         ring[(j + W - 1) % W] = load_frag(tile, next, j + W - 1);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (PINNED) mfma32_settle_vgpr(sacc, pacc);
       // lane = query qi; register r = key k0 + 32ks + 8*(r/4) + 4g + r%4
       // masking in the blocks that straddle the diagonal only (a wave-uniform branch, kept as one)
       if (k0 + 32 * ks + 31 > qw0) {
@@ -926,14 +942,20 @@ __device__ __forceinline__ void attn_bwd_dq(DqLds<D>& lds, int qt, int s, int d,
         __syncthreads();
       }
       __builtin_amdgcn_sched_barrier(0);
+      if constexpr (PINNED) asm volatile("s_nop 1" : "+v"(dsf[0]), "+v"(dsf[1]));
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const int j = ks * HALF + NS + i;
-        dqacc[i % DT] = mfma32(ring[j % W], dsf[i / DT], dqacc[i % DT]);
+        if constexpr (PINNED) mfma32_agpr(dqacc[i % DT], ring[j % W], dsf[i / DT]);
+        else dqacc[i % DT] = mfma32(ring[j % W], dsf[i / DT], dqacc[i % DT]);
         ring[(j + W - 1) % W] = load_frag(tile, next, j + W - 1);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+  }
+  if constexpr (PINNED) {
+#pragma unroll
+    for (int dt = 0; dt < DT; dt += 2) mfma32_settle_agpr(dqacc[dt], dqacc[dt + 1]);
   }
   if (n_own < n_kt) {
     asm volatile("s_barrier" : : : "memory");

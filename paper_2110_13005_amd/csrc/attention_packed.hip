@@ -303,14 +303,14 @@ __global__ __launch_bounds__(256) void attn_packed_dkdv_join_kernel(PackedArgs p
     *reinterpret_cast<elemx4*>(out + col) = v;
   }
 }
-template <int D, int FORM_DELTA>
+template <int D, int FORM_DELTA, bool PINNED>
 __device__ __forceinline__ void packed_dq(DqLds<D>& lds, const PackedArgs& p, uint32_t id) {
   const PackedTile t = packed_tile(p, id, p.heads, p.heads_recip);
   const int head = packed_head(p, t.unit), kv = host::recip_div(head, p.group, p.group_recip);
   if (!t.exists(p.T)) return;
   const PackedHead h = packed_rows(p, t.start, head, kv);
   const int64_t stat = (int64_t)head * p.T + h.row, col = (int64_t)head * p.d;
-  attn_bwd_dq<D, true, FORM_DELTA>(lds, t.tile, t.len, p.d, p.scale, h.q, h.k, h.v, p.ld, p.o + h.row * p.ld_o + col, p.ld_o,
+  attn_bwd_dq<D, true, FORM_DELTA, PINNED>(lds, t.tile, t.len, p.d, p.scale, h.q, h.k, h.v, p.ld, p.o + h.row * p.ld_o + col, p.ld_o,
                                    p.dout + h.row * p.ld_do + col, p.ld_do, p.lse + stat, p.delta + stat,
                                    p.dqkv + h.row * p.ld_dqkv + col, p.ld_dqkv, 0);
 }
@@ -320,16 +320,16 @@ __global__ __launch_bounds__(256) void attn_packed_bwd_dkdv_kernel(PackedArgs p)
   packed_dkdv<D>(lds, p, blockIdx.x);
 }
 template <int D>
-__global__ __launch_bounds__(256, D > 128 ? 1 : 2) void attn_packed_bwd_dq_kernel(PackedArgs p) {
+__global__ __launch_bounds__(256, 2) void attn_packed_bwd_dq_kernel(PackedArgs p) {
   __shared__ DqLds<D> lds;
-  packed_dq<D, FORM_DELTA_ANY>(lds, p, blockIdx.x);
+  packed_dq<D, FORM_DELTA_ANY, false>(lds, p, blockIdx.x);
 }
 // Both at once, for problems whose tiles do not fill the chip: the first workgroups form dK and dV, the others dQ.
 template <int D>
 __global__ __launch_bounds__(256) void attn_packed_bwd_both_kernel(PackedArgs p, uint32_t n_dkdv) {
   __shared__ union { DkdvLds<D> dkdv; DqLds<D> dq; } lds;
   if (blockIdx.x < n_dkdv) packed_dkdv<D>(lds.dkdv, p, blockIdx.x);
-  else packed_dq<D, READ_DELTA>(lds.dq, p, blockIdx.x - n_dkdv);
+  else packed_dq<D, READ_DELTA, (D > 128)>(lds.dq, p, blockIdx.x - n_dkdv);
 }
 
 // delta[head][row] = sum over the head's columns of dO o, for the one-launch backward: LANES lanes per (row, head), 8 elements each,
@@ -395,11 +395,20 @@ uint64_t attention_packed_bwd_ws_bytes(const PackedShape& s) {
   return delta_bytes(s) + (parts > 1 ? (uint64_t)packed_tiles_bound(s.T, s.n_seq) * s.kv * parts * 128 * 2 * packed_columns(s.d) * 4 : 0);
 }
 
-#define AXONN_PACKED(KERNEL, GRID, ...)                                                                     \
+#define AXONN_PACKED_128(KERNEL, GRID, ...)                                                                 \
   do {                                                                                                 \
     if (s.d <= 64) hipLaunchKernelGGL(KERNEL<64>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);          \
-    else if (s.d <= 128) hipLaunchKernelGGL(KERNEL<128>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);   \
-    else hipLaunchKernelGGL(KERNEL<192>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);                   \
+    else hipLaunchKernelGGL(KERNEL<128>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);                   \
+    const hipError_t e = hipGetLastError();                                                            \
+    if (e != hipSuccess) return e;                                                                     \
+  } while (0)
+#define AXONN_PACKED(KERNEL, GRID, ...)                                                                     \
+  do {                                                                                                 \
+    if (s.d <= 128) {                                                                                  \
+      AXONN_PACKED_128(KERNEL, GRID, __VA_ARGS__);                                                     \
+      break;                                                                                           \
+    }                                                                                                  \
+    hipLaunchKernelGGL(KERNEL<192>, dim3(GRID), dim3(256), 0, st, __VA_ARGS__);                        \
     const hipError_t e = hipGetLastError();                                                            \
     if (e != hipSuccess) return e;                                                                     \
   } while (0)
@@ -432,12 +441,13 @@ hipError_t launch_attention_packed_bwd(const PackedShape& s, const void* plan, c
     AXONN_PACKED(attn_packed_delta_kernel, (unsigned)((s.T * s.heads + per_block - 1) / per_block), p);
     AXONN_PACKED(attn_packed_bwd_both_kernel, n_dq + n_dkdv, p, n_dkdv);
   } else {
-    AXONN_PACKED(attn_packed_bwd_dq_kernel, n_dq, p);       // forms delta
-    AXONN_PACKED(attn_packed_bwd_dkdv_kernel, n_dkdv, p);
+    AXONN_PACKED_128(attn_packed_bwd_dq_kernel, n_dq, p);   // forms delta
+    AXONN_PACKED_128(attn_packed_bwd_dkdv_kernel, n_dkdv, p);
   }
   if (p.parts > 1) AXONN_PACKED(attn_packed_dkdv_join_kernel, n_join * (packed_columns(s.d) / 16), p);
   return hipSuccess;
 }
 #undef AXONN_PACKED
+#undef AXONN_PACKED_128
 
 }  // namespace axonn
