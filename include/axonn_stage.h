@@ -626,7 +626,7 @@ int axonn_attention_packed_bwd(int64_t T, int32_t n_seq, int32_t n_heads, int32_
 
 /* Of logits [T, V]: logp[t] = z[target] - lse, lse[t] = log sum_v exp(z[v]), both float32.  A token
  * whose target is outside [0, V) has no part: its row is not read, logp and lse are 0.
- * T <= 2^22, V <= 2^20, here and in the losses below. */
+ * T <= 2^21, V <= 2^20, T * V <= 2^36, here and in the losses below. */
 int axonn_token_logprobs_fwd(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_logits,
                              const int32_t* targets, float* logp, float* lse, void* hip_stream);
 /* Its gradient: dlogits = dlogp[t] (onehot(target) - softmax(z)); rows of zeros for tokens without a

@@ -529,8 +529,8 @@ __global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void distill_loss_ker
   }
 }
 
-// out[0] = scale * sum of x[i] * (weight ? weight[i] : 1): one workgroup, fixed order, 64-bit sums.  What a weight of 0 takes out is
-// finite: such tokens' losses are 0.
+// out[0] = scale * sum of x[i] * (weight ? weight[i] : 1): one workgroup, fixed order, 64-bit sums.  Losses of 0 add nothing, whatever
+// their weight is: they are also those of tokens that have no part.
 __global__ __launch_bounds__(1024) void weighted_sum_kernel(int n, const float* __restrict__ x, const float* __restrict__ weight, float scale,
                                                             float* __restrict__ out) {
   __shared__ double shared[16];
@@ -546,7 +546,7 @@ __global__ __launch_bounds__(1024) void weighted_sum_kernel(int n, const float* 
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (i + j * 1024 < n) s += (double)v[j] * w[j];
+      if (i + j * 1024 < n && v[j] != 0.f) s += (double)v[j] * w[j];
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);

@@ -39,7 +39,8 @@ int packed_ld(const char* what, int64_t width, int64_t ld) {
 
 int logits_shape(const char* what, int64_t T, int64_t V, int64_t ld) {
   if (T < 1 || V < 1) return fail_entry(AXONN_EINVAL, "%s: non-positive size", what);
-  if (T > (1 << 22) || V > (1 << 20)) return fail_entry(AXONN_EUNSUPPORTED, "%s: at most 2^22 rows and a vocabulary of 2^20", what);
+  if (T > (1 << 21) || V > (1 << 20) || T * V > (int64_t(1) << 36))
+    return fail_entry(AXONN_EUNSUPPORTED, "%s: at most 2^21 rows, a vocabulary of 2^20 and 2^36 logits", what);
   if (ld < V) return fail_entry(AXONN_EINVAL, "%s: ld_logits < V", what);
   return AXONN_OK;
 }

@@ -16,7 +16,7 @@ pytestmark = [pytest.mark.gpu, pytest.mark.parametrize("axonn_elem", ["bf16", "f
 # rows, vocabulary, leading dimension, first element
 SIZES = [(1, 1, 1, 0), (3, 2, 5, 1), (4, 7, 7, 0), (5, 8, 8, 0), (6, 9, 12, 3), (3, 255, 255, 1), (9, 1000, 1000, 0), (4, 2047, 2050, 1), (4, 2049, 2049, 0),
          (3, 4100, 4104, 8), (5, 8191, 8191, 0), (2, 16392, 16392, 0), (3, 12289, 12289, 0), (3, 32003, 32003, 1), (2, 40968, 40968, 0), (2, 51200, 51200, 0), (2, 65536, 65536, 0), (2, 70001, 70004, 1), (1, 81921, 81921, 0), (1, 106497, 106497, 3), (1, 131071, 131071, 0),
-         (2, 131080, 131080, 0), (1, 262144, 262144, 0), (1, 300007, 300007, 1)]
+         (2, 131080, 131080, 0), (1, 262144, 262144, 0), (1, 300007, 300007, 1), (1, 393216, 393216, 0)]
 
 
 def f32(x):
@@ -287,6 +287,13 @@ def test_nan_reaches_its_own_row_alone():
     ids = dev_i32((L.targets[:, None] + np.arange(3)) % V)
     B.axonn_distill_loss(T, V, 3, L.buf.t, V, f32(np.zeros((T, 3))), ids, 3, f32(np.full(T, 2.0)), 1.0, ones, 1.0, token, loss, L.grad.t, V)
     assert (torch.isfinite(token) == ~bad).all() and (torch.isfinite(L.grad.t).all(dim=1) == ~bad).all()
+    # tokens without a part: NaN in their rows and in what comes with them reaches nothing
+    labels, w = dev_i32(np.where(bad.cpu().numpy(), -100, L.targets)), torch.where(bad, float("nan"), 1.0)
+    B.axonn_policy_loss(T, V, L.buf.t, V, labels, w, w, w, w, 0.2, 0.2, 0.1, 1.0, logp, token, loss, L.grad.t, V)
+    assert all(torch.isfinite(x).all() for x in (logp, token, loss, L.grad.t)) and (L.grad.t[bad] == 0).all() and (L.grad.t[~bad] != 0).any()
+    none = torch.where(bad[:, None], -1, ids).contiguous()
+    B.axonn_distill_loss(T, V, 3, L.buf.t, V, w[:, None].repeat(1, 3).contiguous(), none, 3, w + 2, 1.0, torch.ones_like(w), 1.0, token, loss, L.grad.t, V)
+    assert all(torch.isfinite(x).all() for x in (token, loss, L.grad.t)) and (L.grad.t[bad] == 0).all()
 
 
 def test_losses_captured():

@@ -73,19 +73,20 @@ def logits(fn, ok, T=0, V=1, ld=3):
     each(INV, fn, ok, {T: (0, -1), V: (0, -1)})
     if ld is not None:
         refused(INV, fn, *with_args(ok, **{"_%d" % ld: ok[V] - 1}))
-    refused(UNS, fn, *with_args(ok, **{"_%d" % T: (1 << 22) + 1}))
+    refused(UNS, fn, *with_args(ok, **{"_%d" % T: (1 << 21) + 1}))
     refused(UNS, fn, *with_args(ok, **({"_%d" % V: (1 << 20) + 1, "_%d" % ld: 1 << 21} if ld is not None else {"_%d" % V: (1 << 20) + 1})))
 
 
 def test_token_logprobs():
     ok = [4, 10, A, 10, A, A, A]
     nulls(B.axonn_token_logprobs_fwd, ok, (2, 4, 5, 6))
+    refused(UNS, B.axonn_token_logprobs_fwd, *with_args(ok, _0=1 << 21, _1=(1 << 15) + 1, _3=1 << 16))
     logits(B.axonn_token_logprobs_fwd, ok)
     ok = [4, 10, A, 10, A, A, A, A, 10]
     nulls(B.axonn_token_logprobs_bwd, ok, (2, 4, 5, 6, 7))
     logits(B.axonn_token_logprobs_bwd, ok)
     each(INV, B.axonn_token_logprobs_bwd, ok, {8: (9, 11)})                    # too small; in place with another one
-    assert "T <= 2^22, V <= 2^20" in comment_of("axonn_token_logprobs_fwd")
+    assert "T <= 2^21, V <= 2^20, T * V <= 2^36" in comment_of("axonn_token_logprobs_fwd")
 
 
 def test_policy_loss():
