@@ -190,12 +190,14 @@ def load(elem=None):
 
 def _ptr(x):
     """torch tensor / numpy array / int / None -> address."""
-    if x is None:
-        return None
+    if x is None or x.__class__ is int:
+        return x
+    try:
+        return x.data_ptr()          # most are tensors: a call with a dozen of them is several microseconds of host time
+    except AttributeError:
+        pass
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if hasattr(x, "ctypes"):
         return x.ctypes.data
     if isinstance(x, C.c_void_p):

@@ -110,6 +110,7 @@ __device__ __forceinline__ T* chunk_of(T* row, uint32_t chunk) {
 
 // A row of logits in the registers of a workgroup: thread t of THREADS holds chunks t, t + THREADS, ... of 8, as many as it takes
 // (so all but the last, or the last two where there is no kernel for every number, are whole: the first WHOLE).
+constexpr int row_waves(int chunks) { return chunks >= 1 && chunks <= 8 ? 8 : 4; }      // waves per SIMD that registers are shared among
 constexpr int row_whole(int chunks) { return chunks <= 8 ? chunks - 1 : chunks - 2; }
 template <int THREADS, int CHUNKS, int WHOLE = row_whole(CHUNKS)>
 struct Row {
@@ -168,15 +169,26 @@ struct Row {
     if (tid == (column >> 3) % THREADS) out[column] = (elem_t)value;
   }
 };
-// A row that is too long for them: read for its statistics, with the running-maximum recurrence, and once more for the gradient.
+// A row that is too long for them: what registers do not hold is read for the statistics, with the running-maximum recurrence, and once
+// more for the gradient.
 template <int THREADS>
 struct Row<THREADS, 0, -1> {
-  static constexpr int AT_ONCE = 4;
+  static constexpr int HEAD = 16, FIRST = 8 * THREADS * HEAD, AT_ONCE = 4;
+  Row<THREADS, HEAD, HEAD> head;                      // columns up to FIRST; what follows is the rest's
   const elem_t* row;
   const uint8_t* named;
   int V, tid;
-  __device__ __forceinline__ void load(const elem_t* row_, int V_, int tid_) { row = row_; V = V_; tid = tid_; named = nullptr; }
-  __device__ __forceinline__ void without(const uint8_t* named_, int, int) { named = named_; }
+  __device__ __forceinline__ void load(const elem_t* row_, int V_, int tid_) {
+    head.load(row_, V_, tid_);
+    row = row_;
+    V = V_;
+    tid = tid_;
+    named = nullptr;
+  }
+  __device__ __forceinline__ void without(const uint8_t* named_, int, int) {
+    head.without(named_, V, tid);
+    named = named_;
+  }
   __device__ __forceinline__ void chunks(int first, elemx8 (&v)[AT_ONCE]) const {
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j) {
@@ -191,9 +203,9 @@ struct Row<THREADS, 0, -1> {
       }
     }
   }
-  __device__ __forceinline__ RowStats stats(float c, RowShared<THREADS>& shared) const {
+  __device__ __forceinline__ RowStats stats(float c, RowShared<THREADS>& shared) {
     float m = -INFINITY, sum = 0.f;
-    for (int at = 8 * tid; at < V; at += 8 * THREADS * AT_ONCE) {
+    for (int at = FIRST + 8 * tid; at < V; at += 8 * THREADS * AT_ONCE) {
       elemx8 v[AT_ONCE];
       chunks(at, v);
       const float old = m;
@@ -207,12 +219,17 @@ struct Row<THREADS, 0, -1> {
         for (int i = 0; i < 8; ++i) part += __builtin_amdgcn_exp2f(((float)v[j][i] - from) * c);
       sum = sum * __builtin_amdgcn_exp2f((old - from) * c) + part;
     }
-    const Exponent e(block_all<THREADS>(m, shared.max, OpMax()), c);
-    sum = block_all<THREADS>(sum * __builtin_amdgcn_exp2f((m - e.m) * c), shared.sum, OpSum());
-    return RowStats{e, sum * __builtin_amdgcn_exp2f(e.low)};
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < HEAD; ++j) top = chunk_max(top, head.v[j]);
+    const Exponent e(block_all<THREADS>(top, shared.max, OpMax()), c);
+    // the rest's sum is of exponentials without the common factor
+    sum = head.sum(e) + sum * __builtin_amdgcn_exp2f((m - e.m) * c) * __builtin_amdgcn_exp2f(e.low);
+    return RowStats{e, block_all<THREADS>(sum, shared.sum, OpSum())};
   }
-  __device__ __forceinline__ void store(elem_t* out, int, int, const Exponent& e, float f) const {
-    for (int first = 8 * tid; first < V; first += 8 * THREADS * AT_ONCE) {
+  __device__ __forceinline__ void store(elem_t* out, int, int, const Exponent& e, float f) {
+    head.store(out, V, tid, e, f);
+    for (int first = FIRST + 8 * tid; first < V; first += 8 * THREADS * AT_ONCE) {
       elemx8 v[AT_ONCE];
       chunks(first, v);
 #pragma unroll
@@ -234,7 +251,7 @@ __device__ __forceinline__ void store_zeros(elem_t* out, int V, int tid) {
 }
 
 template <int THREADS, int CHUNKS>
-__global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void token_logprobs_fwd_kernel(int V, const elem_t* __restrict__ logits, int64_t ld,
+__global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void token_logprobs_fwd_kernel(int V, const elem_t* __restrict__ logits, int64_t ld,
                                                                      const int* __restrict__ targets, float* __restrict__ logp,
                                                                      float* __restrict__ lse) {
   __shared__ RowShared<THREADS> shared;
@@ -297,7 +314,7 @@ __device__ __forceinline__ void policy_token(const PolicyArgs& p, float logp, fl
   }
 }
 template <int THREADS, int CHUNKS>
-__global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void policy_loss_kernel(PolicyArgs p) {
+__global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void policy_loss_kernel(PolicyArgs p) {
   __shared__ RowShared<THREADS> shared;
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, V = p.V, target = p.targets[t];
@@ -462,7 +479,7 @@ __device__ __forceinline__ void distill_list(const DistillArgs& a, int64_t t, co
 }
 
 template <int THREADS, int CHUNKS>
-__global__ __launch_bounds__(THREADS, CHUNKS <= 8 ? 8 : 4) void distill_loss_kernel(DistillArgs a) {
+__global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kernel(DistillArgs a) {
   extern __shared__ uint32_t named[];                 // a bit per token of the vocabulary: the teacher has named it
   __shared__ DistillList list;
   __shared__ RowShared<THREADS> shared;
