@@ -173,6 +173,10 @@ struct TileSource {
   }
 };
 
+// Elements of a result tile as an operand of the next product: probabilities and dS are rounded to 16 bits here, because the matrix
+// unit takes no wider ones at its full rate.  Sums of them are off by about one more rounding of the result: 2.0e-3 of the output in
+// the root mean square where the last rounding alone is 1.6e-3 (bfloat16), 2.4e-3 to 2.6e-3 of the gradients, which the rounded o in delta
+// reaches too (more so in short sequences).  Maxima, sums and log-sum-exps are fp32, of unrounded probabilities.
 __device__ __forceinline__ elemx8 pack8(const floatx16& t, int first) {
   elemx8 o;
 #pragma unroll
@@ -240,6 +244,10 @@ __device__ __forceinline__ void store_rows_out(char* lds, const floatx16* acc, f
 // Against tiles fetched into registers, stored between two barriers, and each tile's fragments read in one go, us: 40 heads of
 // 128 x 2048 58.0 -> 52.0, 16 of 128 x 8192 311 -> 278 (990 TFLOP/s), 8 x 16 of 64 x 1024 28.4 -> 27.1, 8 x 24 of 188 x 512 (every
 // lane on a row of its own, 8 bytes at a time) 76 -> 50.6, 2 x 36 of 176 x 2048 256 -> 153.
+// KEYS: rows of a key tile.  With 32 and fewer fragments on their way two workgroups of 192 columns share a CU (254 registers), where 64
+// leave one with 482, between whose two kinds the compiler moves values throughout the loop: 24 heads of 188, seven sequences of about 512,
+// 46 -> 34 us, 2 x 36 of 176 x 2048 154 -> 123.  At 128 columns, where two share it either way, tiles of 32 are slower (40 heads, seven
+// sequences of 80 to 1023, 52.6 -> 54.2; 16 of 8192 267 -> 278), and three workgroups per CU spill.
 template <int D, int KEYS = 64>
 struct FwdLds {
   static constexpr int BKV = KEYS, BUF = 2 * Tile<BKV, D>::BYTES;
@@ -736,8 +744,8 @@ __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, in
 // `delta` is read and `o` ignored.  by_4: the sums in the order of the launch of its own, for sequences that take that launch
 // when they do not run with others.  FORM_DELTA_ANY: for any d, in an order of its own.
 // PINNED: the accumulators in the accumulation registers, scores and all operands in ordinary ones, by assembly (see mfma32_agpr); for
-// a wave that is alone on its SIMD.  The compiler, which gives every MFMA of such a kernel accumulation registers, moves a quarter of what the
-// loop issues between the two kinds otherwise.
+// a wave that is alone on its SIMD.  The compiler, which gives every MFMA of such a kernel accumulation registers, otherwise moves values
+// between the two kinds for a sixth of what the loop issues.  Backward of 2 x 36 heads of 176 x 2048 489 -> 477 us.
 //
 // Two workgroups share a CU.  The fragments run a few MFMAs ahead through a ring, so that a wave waits for LDS only behind the
 // two barriers of a tile: one when everybody has left the tile before, whose buffer the memory pipeline then fills, one when

@@ -241,6 +241,10 @@ __device__ __forceinline__ PackedHead packed_rows(const PackedArgs& p, int start
   return h;
 }
 
+// MFMA-bound on long sequences: one of 8192, 16 heads of 128 on 4, 267 us (1030 TFLOP/s of algorithmic work; the matrix units are busy 64 %
+// of the time, at the clock that the power limit leaves).  On shorter ones the tiles' beginnings and ends count: of 40 heads of 128 over
+// sequences of 80 to 1023 rows (4003 in all, 53 us, 600 TFLOP/s) the matrix units are busy 35 %; a workgroup walks 7 tiles of keys on
+// average, about 1 us each, and takes 5 to get its rows, to leave its results and to give way to the next.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_packed_fwd_kernel(PackedArgs p) {
   constexpr int KEYS = D > 128 ? 32 : 64;
@@ -266,7 +270,8 @@ __device__ __forceinline__ void packed_dkdv(DkdvLds<D>& lds, const PackedArgs& p
                                dk + (int64_t)p.kv * p.d, p.ld_dqkv, heads, p.T,
                                p.parts > 1 ? p.partial + (int64_t)id * partial_size<D>() : nullptr);
 }
-// The parts' sums: a workgroup per tile, key / value head, dK or dV and 32 columns; a lane has 32 columns' half of a row.
+// The parts' sums, in order: a workgroup per tile, key / value head, dK or dV and 32 columns; a lane has 32 columns' half of a row.  What
+// it takes is the latency of its reads and HBM: 2 parts of 64 tiles x 4 heads of 128 columns, 67 MB, 17 us.
 template <int D>
 __global__ __launch_bounds__(256) void attn_packed_dkdv_join_kernel(PackedArgs p) {
   constexpr int DT = D / 32, AT_ONCE = 4;
@@ -314,6 +319,9 @@ __device__ __forceinline__ void packed_dq(DqLds<D>& lds, const PackedArgs& p, ui
                                    p.dout + h.row * p.ld_do + col, p.ld_do, p.lse + stat, p.delta + stat,
                                    p.dqkv + h.row * p.ld_dqkv + col, p.ld_dqkv, 0);
 }
+// dK / dV in a launch of its own behind dQ (up to 128 columns).  One sequence of 8192, 16 heads of 128 on 4: dQ 375, dK / dV 500, the parts' sums
+// 17 us, 850 together (810 TFLOP/s; matrix units busy 65 % in both); the 40 heads above 73, 112 and none, busy 37 %: of a workgroup's 20 us
+// 6.5 go to its beginning and end, which nothing hides (one workgroup per CU: 362 registers, 130 KB of LDS).
 template <int D>
 __global__ __launch_bounds__(256) void attn_packed_bwd_dkdv_kernel(PackedArgs p) {
   __shared__ DkdvLds<D> lds;
@@ -324,7 +332,8 @@ __global__ __launch_bounds__(256, 2) void attn_packed_bwd_dq_kernel(PackedArgs p
   __shared__ DqLds<D> lds;
   packed_dq<D, FORM_DELTA_ANY, false>(lds, p, blockIdx.x);
 }
-// Both at once, for problems whose tiles do not fill the chip: the first workgroups form dK and dV, the others dQ.
+// Both at once (host::packed_one_launch): the first workgroups form dK and dV, the others dQ.  24 heads of 188 over seven sequences of about
+// 512: 110 us where the two launches took 63 and 72.
 template <int D>
 __global__ __launch_bounds__(256) void attn_packed_bwd_both_kernel(PackedArgs p, uint32_t n_dkdv) {
   __shared__ union { DkdvLds<D> dkdv; DqLds<D> dq; } lds;
@@ -333,7 +342,7 @@ __global__ __launch_bounds__(256) void attn_packed_bwd_both_kernel(PackedArgs p,
 }
 
 // delta[head][row] = sum over the head's columns of dO o, for the one-launch backward: LANES lanes per (row, head), 8 elements each,
-// DELTA_PAIRS pairs on their way at once.
+// DELTA_PAIRS pairs on their way at once.  HBM-bound: 3064 rows of 24 heads of 188, 55 MB, 12 us.
 constexpr int DELTA_PAIRS = 4;
 template <int D>
 __global__ __launch_bounds__(256) void attn_packed_delta_kernel(PackedArgs p) {
