@@ -654,6 +654,7 @@ int axonn_policy_loss(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_
  * the margin m = beta (sum over the chosen - sum over the rejected tokens of (logp - ref_logp)):
  *   pair_loss[i] = -(1 - label_smoothing) log sigma(m) - label_smoothing log sigma(-m)
  *   loss[0] = scale sum_i pair_loss[i],   dlogp[t] = loss_scale d loss / d logp[t]
+ * (a term whose factor is 0 has no part, so that without smoothing an infinite margin has the loss 0 or infinity).
  * Tokens whose target is outside [0, V) have no part, like those that belong to no sequence: dlogp is 0
  * there.  The sums over tokens are formed in 64 bits.  ref_logp (NULL: zeros) and loss may be NULL.
  * axonn_token_logprobs_fwd in front and _bwd behind make it a loss over logits. */

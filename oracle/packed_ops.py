@@ -107,7 +107,7 @@ def preference_loss(logp, ref_logp, offsets, live, beta, smoothing, scale):
     for (a, b), (c, d) in zip(spans[0::2], spans[1::2]):
         m = beta * (x[a:b].sum() - x[c:d].sum())
         sigma = 1 / (1 + np.exp(-m))
-        losses.append((1 - smoothing) * np.logaddexp(0, -m) + smoothing * np.logaddexp(0, m))
+        losses.append(sum(share * np.logaddexp(0, side) for share, side in ((1 - smoothing, -m), (smoothing, m)) if share > 0))
         slope = scale * beta * (smoothing * sigma - (1 - smoothing) * (1 - sigma))
         dlogp[a:b], dlogp[c:d] = slope, -slope
     return np.array(losses), scale * float(np.sum(losses)), np.where(live, dlogp, 0.0)

@@ -394,12 +394,12 @@ __global__ __launch_bounds__(PREF_THREADS) void preference_loss_kernel(Preferenc
       rejected = wave_sum64(lane < WAVES ? shared[1][lane] : 0.0);
     }
     const float m = (float)((double)p.beta * (chosen - rejected));
-    // -log sigma(m) = max(-m, 0) + log(1 + exp(-|m|))
-    const float tail = log1pf(expf(-fabsf(m)));
-    const float value = (1.f - p.smoothing) * (fmaxf(-m, 0.f) + tail) + p.smoothing * (fmaxf(m, 0.f) + tail);
+    // -log sigma(m) = max(-m, 0) + log(1 + exp(-|m|)); without a share an infinite one (a token of probability 0) has no part
+    const float tail = log1pf(expf(-fabsf(m))), miss = 1.f - p.smoothing;
+    const float value = (miss > 0.f ? miss * (fmaxf(-m, 0.f) + tail) : 0.f) + (p.smoothing > 0.f ? p.smoothing * (fmaxf(m, 0.f) + tail) : 0.f);
     if ((ALL ? lane : tid) == 0) p.pair_loss[pair] = value;
     total += value;
-    const float dm = p.smoothing / (1.f + expf(-m)) - (1.f - p.smoothing) / (1.f + expf(m));
+    const float dm = p.smoothing / (1.f + expf(-m)) - miss / (1.f + expf(m));
     const float slope = p.scale * p.loss_scale * p.beta * dm;
     for (int t = first; t < e; t += STEP) p.dlogp[t] = live(t) ? (t < b ? slope : -slope) : 0.f;
   }

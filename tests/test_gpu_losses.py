@@ -160,6 +160,22 @@ def test_preference_loss(lens, front, pad, smoothing):
         assert not host(d)[~live].any() and not host(d)[:front].any() and not host(d)[T - pad:].any()
 
 
+@pytest.mark.parametrize("rows", [4, 2000])                       # one workgroup, and one per pair
+@pytest.mark.parametrize("smoothing,want", [(0.0, [0.0, np.inf]), (1.0, [np.inf, 0.0]), (0.25, [np.inf, np.inf])])
+def test_preference_of_a_token_without_probability(rows, smoothing, want):
+    """A log-probability of -inf in the rejected or the chosen answer: an infinite margin, saturated gradients."""
+    logp = np.full(rows, -1.0, np.float32)
+    off = np.array([0, 1, rows // 2, rows - 1, rows])                # pair 0: rejected has it; pair 1: chosen
+    logp[1] = logp[rows // 2] = -np.inf
+    pair, loss, d = empty(2), empty(1), empty(rows)
+    B.axonn_preference_loss(rows, 2, 9, dev_i32(off), dev_i32(np.zeros(rows)), f32(logp), None, 0.5, smoothing, 1.0, 1.0, pair, loss, d)
+    assert host(pair).tolist() == want and host(loss)[0] == np.inf
+    # d loss / dm: smoothing - (1 - smoothing) 0 at +inf, smoothing 0 - (1 - smoothing) at -inf
+    slope = np.where(np.arange(rows) < rows // 2, 0.5 * smoothing, -0.5 * (1 - smoothing))
+    chosen = (np.arange(rows) < 1) | ((np.arange(rows) >= rows // 2) & (np.arange(rows) < rows - 1))
+    assert (host(d) == np.where(chosen, slope, -slope)).all()
+
+
 class Teacher:
     def __init__(self, L, K, tail, how):
         rng, T, V = L.rng, L.T, L.V

@@ -87,6 +87,10 @@ def test_preference_gradient(smoothing):
     assert np.allclose(d, differences(lambda x: P.preference_loss(x, ref, off, live, 0.5, smoothing, 0.7)[1], logp), atol=1e-9)
     same = P.preference_loss(logp, logp, off, live, 0.5, smoothing, 1.0)
     assert np.allclose(same[0], np.log(2))
+    # a rejected token without probability: nothing left to prefer, unless the labels are smoothed
+    logp[4], live = -np.inf, np.ones(11, bool)
+    pair, _, d = P.preference_loss(logp, ref, off, live, 0.5, smoothing, 0.7)
+    assert pair[0] == (np.inf if smoothing else 0.0) and np.allclose(d[1:6], 0.35 * smoothing * np.array([1, 1, 1, -1, -1]))
 
 
 @pytest.mark.parametrize("tail", [False, True])
