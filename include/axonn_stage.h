@@ -671,7 +671,8 @@ int axonn_preference_loss(int64_t T, int32_t n_pairs, int64_t V, const int32_t* 
  *                      token_loss = sum_j p_j (log p_j - log q_j)
  *   else               p_j = exp(teacher_logits_j / temperature - teacher_lse[t]), and the mass of all other
  *                      tokens is one more outcome: + P (log P - log Q), P = max(1 - sum_j p_j, 0),
- *                      Q = the student's mass of the tokens that are not named
+ *                      Q = the student's mass of the tokens that are not named (no such term where Q
+ *                      is 0: all tokens are named, or the others' logits are -infinity)
  *   loss[0] = sum_t weight[t] token_loss[t],   dlogits = loss_scale d loss / d logits
  * A token named twice counts as two entries.  Rows in which no token is named, or whose weight is 0, have
  * no part: token_loss 0, dlogits zeros.  loss may be NULL; so may dlogits, or it

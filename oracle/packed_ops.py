@@ -136,8 +136,9 @@ def distill_loss(logits, teacher, ids, teacher_lse, temperature, weight):
             P = max(1.0 - sum(np.exp(x - norm) for _, x in entries), 0.0)
             if P > 0:
                 top = logq[others].max() if others.any() else -np.inf
-                logQ = top + np.log(np.exp(logq[others] - top).sum()) if np.isfinite(top) else -np.inf
-                loss[t] += P * (np.log(P) - logQ)
-                g[others] -= P * np.exp(logq[others] - logQ)
+                if np.isfinite(top):                                   # else the student has no other tokens
+                    logQ = top + np.log(np.exp(logq[others] - top).sum())
+                    loss[t] += P * (np.log(P) - logQ)
+                    g[others] -= P * np.exp(logq[others] - logQ)
         dz[t] = weight[t] / temperature * g
     return loss, float(np.sum(np.asarray(weight, np.float64) * loss)), dz

@@ -3,8 +3,8 @@
 //
 // With q = softmax(z), every gradient is a multiple of q plus a few elements of its own:
 //   d log q_t / dz = onehot_t - q
-// HBM-bound: a row of logits is read once and its gradient written once.  A workgroup holds the row in registers between the two (vocabularies
-// of up to 65536; longer rows are read twice).  Tokens without a part are not read.
+// HBM-bound: a row of logits is read once and its gradient written once.  A workgroup holds the row in registers between the two (up to 131072
+// columns; what lies behind them is read twice).  Tokens without a part are not read.
 #include "rows.h"
 #include "host_logic.h"
 #include <type_traits>
@@ -530,7 +530,8 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
   if (a.teacher_lse) {
     rest = 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;
-    if (rest != 0.f) loss += rest * (logf(rest) - ((r.e.m - m) * per + logf(r_sum) - log_all));
+    // (all tokens named, or the others masked: what 1 - mass is then is its rounding, which would count infinitely)
+    if (rest != 0.f && r_sum != 0.f) loss += rest * (logf(rest) - ((r.e.m - m) * per + logf(r_sum) - log_all));
   }
   if (tid == 0) a.token_loss[t] = loss;
   if (!a.dlogits) return;

@@ -10,7 +10,7 @@ from oracle import packed_ops as P
 from paper_2110_13005_amd import binding as B
 from paper_2110_13005_amd.inputs import snap_elem
 from helpers import dev_i32, host
-from test_gpu_step_ops import Padded, U, normal, within
+from test_gpu_step_ops import Padded, U, half_step, normal, within
 
 pytestmark = [pytest.mark.gpu, pytest.mark.parametrize("axonn_elem", ["bf16", "fp16"], indirect=True)]
 # rows, vocabulary, leading dimension, first element
@@ -251,6 +251,39 @@ def test_distill_loss(T, V, ld, shift, how, tail):
     B.axonn_distill_loss(T, V, K, L.buf.t, ld, *ops, token2, loss, L.buf.t, ld)
     assert (L.buf.t == before).all() and (token2 == token).all()
     L.buf.result()
+
+
+@pytest.mark.parametrize("V", [1, 7, 64, 300, 1024])
+@pytest.mark.parametrize("masked", [False, True])
+def test_distill_of_all_tokens(V, masked):
+    """All tokens that have a probability are named: with the teacher's own log-sum-exp, however it is rounded, as without one."""
+    import torch
+    T, W, tau = 6, V + 77 * masked, 1.5
+    L = Logits(T, V, masked=0.0)
+    buf = torch.full((T, W), float("-inf"), dtype=L.buf.t.dtype, device="cuda")
+    buf[:, :V] = L.buf.t
+    ids = np.stack([L.rng.permutation(V) for _ in range(T)])
+    u = L.rng.standard_normal((T, V)).astype(np.float32)
+    top = u.max(axis=1).astype(np.float64) / tau
+    lse = top + np.log(np.sum(np.exp(u.astype(np.float64) / tau - top[:, None]), axis=1))
+    w = f32(np.ones(T))
+    got = []
+    for x in (None, *(f32(lse.astype(np.float32) + i * np.spacing(np.abs(lse).astype(np.float32))) for i in (-1, 0, 1))):
+        token, grad = empty(T), torch.zeros_like(buf)
+        B.axonn_distill_loss(T, W, V, buf, W, f32(u), dev_i32(ids), V, x, tau, w, 1.0, token, None, grad, W)
+        got.append((host(token), host(grad)))
+    # the two log-sum-exps: one and a half steps of the given one; the formed one's exponents, sum and logarithm
+    delta = U * (3 * np.abs(lse) + 4 * np.abs(top) + V / 64 + 20 + 3 * (top[:, None] - u / tau).max(axis=1))[:, None]
+    p, logp = np.exp(u / tau - lse[:, None]), u / tau - lse[:, None]
+    logq = np.take_along_axis(P.log_softmax(L.z / tau), ids, axis=1)
+    gap = np.abs(np.take_along_axis(L.z, ids, axis=1) - L.z.max(axis=1, keepdims=True)) / tau
+    slack = np.sum(p * (delta * (np.abs(logp - logq) + 1) + 2 * U * (V / 64 + 24) * (np.abs(logp) + gap + np.abs(logq) + 1)), axis=1)
+    full = np.zeros((T, W))
+    np.put_along_axis(full, ids, p * delta / tau, axis=1)
+    for token, grad in got[1:]:
+        assert (np.abs(token - got[0][0]) <= 2 * slack).all()
+        assert (np.abs(grad - got[0][1]) <= 2 * full * (1 + half_step()) + 2 * half_step() * np.abs(got[0][1]) + 4 * U).all()
+        assert not grad[:, V:].any()
 
 
 def test_infinite_and_lowest_logits():

@@ -107,3 +107,7 @@ def test_distillation_gradient(tail):
     ids = np.tile(np.arange(V), (T, 1))
     loss, _, dz = P.distill_loss(z, z, ids, np.log(np.exp(z / 1.5).sum(axis=1)) if tail else None, 1.5, w)
     assert np.allclose(loss, 0, atol=1e-7) and np.allclose(dz, 0, atol=1e-12)
+    # all tokens named with a log-sum-exp that is a little too large: the rest's mass is nobody's
+    lse = np.log(np.exp(u / 1.5).sum(axis=1))
+    few = [P.distill_loss(z[:, :K], u, ids[:, :K], x, 1.5, w)[0] for x in (None, lse + 1e-7)]
+    assert np.allclose(few[0], few[1], atol=1e-5)
