@@ -603,7 +603,8 @@ int axonn_attention_packed_plan(int64_t T, int32_t n_seq, const int32_t* offsets
  * j / (n_heads / n_kv_heads).  With i, j positions in a sequence:
  *   o_i = sum_j<=i P_ij v_j,   P_ij = exp(scale q_i.k_j - lse_i),   lse_i = log sum_j<=i exp(scale q_i.k_j)
  * o [T, n_heads * head_dim]; lse [n_heads][T] float32.  Rows of o and lse that belong to no sequence are
- * left as they are, and nothing that lies in another row than a sequence's reaches its results.
+ * left as they are, and nothing that lies in another row than a sequence's reaches its results.  (Infinities
+ * and NaN in a sequence's own rows can reach rows in front of them: masked zeros are multiplied by them.)
  * head_dim a multiple of 4, at most 192; n_heads a multiple of n_kv_heads, at most 4096;
  * T * n_heads <= 2^27, n_seq * n_heads <= 2^22; leading dimensions at most 2^22; scale > 0
  * (usually 1 / sqrt(head_dim)). */
@@ -657,7 +658,8 @@ int axonn_policy_loss(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_
  * (a term whose factor is 0 has no part, so that without smoothing an infinite margin has the loss 0 or infinity).
  * Tokens whose target is outside [0, V) have no part, like those that belong to no sequence: dlogp is 0
  * there.  The sums over tokens are formed in 64 bits.  ref_logp (NULL: zeros) and loss may be NULL.
- * axonn_token_logprobs_fwd in front and _bwd behind make it a loss over logits. */
+ * axonn_token_logprobs_fwd in front and _bwd behind make it a loss over logits.  (Offsets that do not ascend
+ * are clamped to [0, T] only: pairs then share rows of dlogp.) */
 int axonn_preference_loss(int64_t T, int32_t n_pairs, int64_t V, const int32_t* offsets,
                           const int32_t* targets, const float* logp, const float* ref_logp,
                           float beta, float label_smoothing, float scale, float loss_scale,

@@ -297,8 +297,8 @@ __global__ __launch_bounds__(GRAD_THREADS) void token_logprobs_bwd_kernel(int V,
   const bool here = target >= (int)first && target < (int)first + n;
   const float at_target = here ? (float)logits[t * ld + target] : 0.f;
   if (logits == dlogits) __syncthreads();             // read before it is overwritten
-  // exp(z - lse) with the rounded product's factor taken out
-  const float f = -slope * __builtin_amdgcn_exp2f(-e.low);
+  // exp(z - lse) with the rounded product's factor taken out; a row of nothing but -inf has no softmax, as in the forward pass
+  const float f = lse[t] == -INFINITY ? NAN : -slope * __builtin_amdgcn_exp2f(-e.low);
   row.store(out, n, tid, e, f);
   if (here) row.store_one(out, tid, target - (int)first, e(at_target) * f + slope);
 }

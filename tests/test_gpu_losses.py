@@ -317,6 +317,25 @@ def test_infinite_and_lowest_logits():
         assert (host(token) == 0).all() and (L.grad.result() == 0).all()
 
 
+def test_rows_of_nothing_but_masked_logits():
+    """They have no softmax: NaN in the row's results, whichever way they are formed, and in no other row's."""
+    import torch
+    T, V = 3, 2100
+    L = Logits(T, V, masked=0.0)
+    L.buf.t[1] = -float("inf")
+    t, ones, fine = dev_i32(L.targets), f32(np.ones(T)), torch.tensor([True, False, True]).cuda()
+    logp, lse, token = empty(T), empty(T), empty(T)
+    B.axonn_token_logprobs_fwd(T, V, L.buf.t, V, t, logp, lse)
+    assert (torch.isfinite(logp) == fine).all() and lse[1] == -float("inf")
+    B.axonn_token_logprobs_bwd(T, V, L.buf.t, V, t, lse, ones, L.grad.t, V)
+    assert torch.isfinite(L.grad.t[fine]).all() and torch.isnan(L.grad.t[1]).all()
+    B.axonn_policy_loss(T, V, L.buf.t, V, t, f32(np.full(T, -8)), None, ones, ones, 0.2, 0.2, 0.0, 1.0, None, token, None, L.grad.t, V)
+    assert (torch.isfinite(token) == fine).all() and torch.isfinite(L.grad.t[fine]).all() and torch.isnan(L.grad.t[1]).all()
+    ids = dev_i32(np.tile(np.arange(3), (T, 1)))
+    B.axonn_distill_loss(T, V, 3, L.buf.t, V, f32(np.zeros((T, 3))), ids, 3, None, 1.0, ones, 1.0, token, None, L.grad.t, V)
+    assert (torch.isfinite(token) == fine).all() and torch.isfinite(L.grad.t[fine]).all() and torch.isnan(L.grad.t[1, :3]).all()
+
+
 def test_nan_reaches_its_own_row_alone():
     import torch
     T, V = 6, 3001
