@@ -125,20 +125,21 @@ def distill_loss(logits, teacher, ids, teacher_lse, temperature, weight):
         u = np.array([e[1] for e in entries])
         m = u.max()
         norm = m + np.log(np.exp(u - m).sum()) if teacher_lse is None else float(teacher_lse[t])
-        logq, g = logq_all[t], np.exp(logq_all[t])
-        others = np.ones(V, bool)
+        logq = logq_all[t]
+        others, p = np.ones(V, bool), np.zeros(V)
         for (i, x) in entries:
-            p = np.exp(x - norm)
-            loss[t] += p * (x - norm - logq[i]) if p else 0.0
-            g[i] -= p
+            e = np.exp(x - norm)
+            loss[t] += e * (x - norm - logq[i]) if e else 0.0
+            p[i] += e
             others[i] = False
         if teacher_lse is not None:
-            P = max(1.0 - sum(np.exp(x - norm) for _, x in entries), 0.0)
-            if P > 0:
-                top = logq[others].max() if others.any() else -np.inf
-                if np.isfinite(top):                                   # else the student has no other tokens
-                    logQ = top + np.log(np.exp(logq[others] - top).sum())
-                    loss[t] += P * (np.log(P) - logQ)
-                    g[others] -= P * np.exp(logq[others] - logQ)
+            P = max(1.0 - p.sum(), 0.0)
+            if P > 0 and np.isfinite(logq[others]).any():              # else the student has no other tokens
+                share = log_softmax(np.asarray(logits[t][others], np.float64) / temperature)
+                likely = share.argmax()
+                loss[t] += P * (np.log(P) - (logq[others][likely] - share[likely]))
+                p[others] = P * np.exp(share)
+        # of sum_i p_i (log p_i - log q_i), whatever the p_i sum up to
+        g = p.sum() * np.exp(logq) - p
         dz[t] = weight[t] / temperature * g
     return loss, float(np.sum(np.asarray(weight, np.float64) * loss)), dz

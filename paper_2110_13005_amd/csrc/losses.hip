@@ -526,18 +526,20 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
   const float m = list.sum == 0.f ? r.e.m : r_sum > 0.f ? fmaxf(list.top, r.e.m) : list.top;
   const float others = __builtin_amdgcn_exp2f((r.e.m - m) * c), all = list.sum * __builtin_amdgcn_exp2f((list.top - m) * c) + (r_sum > 0.f ? r_sum * others : r_sum);
   const float log_all = logf(all);
-  float loss = list.gain + list.mass * ((m - list.top) * per + log_all), rest = 0.f;
+  // The others' mass is an outcome of its own, if it has one and the student has other tokens (if not, what 1 - mass is may be its rounding,
+  // which would count infinitely); total: the mass of all outcomes, 1 with that one.
+  float loss = list.gain + list.mass * ((m - list.top) * per + log_all), rest = 0.f, total = 1.f;
   if (a.teacher_lse) {
-    rest = 1.f - list.mass;
+    rest = r_sum == 0.f ? 0.f : 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;
-    // (all tokens named, or the others masked: what 1 - mass is then is its rounding, which would count infinitely)
-    if (rest != 0.f && r_sum != 0.f) loss += rest * (logf(rest) - ((r.e.m - m) * per + logf(r_sum) - log_all));
+    if (rest != 0.f) loss += rest * (logf(rest) - ((r.e.m - m) * per + logf(r_sum) - log_all));
+    else total = list.mass;
   }
   if (tid == 0) a.token_loss[t] = loss;
   if (!a.dlogits) return;
-  // q - p of the named tokens; of the others q (1 - P / Q)
+  // q total - p of the named tokens; of the others q (total - P / Q)
   const float g = w * a.loss_scale * per;
-  const float f = r_sum == 0.f ? 0.f : g * (others / all - rest / r_sum) * __builtin_amdgcn_exp2f(-r.e.low);
+  const float f = r_sum == 0.f ? 0.f : g * (total * others / all - rest / r_sum) * __builtin_amdgcn_exp2f(-r.e.low);
   row.store(out, V, tid, r.e, f);
   __syncthreads();
   if (tid >= 64) return;
@@ -551,7 +553,7 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
       for (int i = j + 1; i < K; ++i)
         if (list.id[i] == id) p += list.p[i];
     }
-    if (first) out[id] = (elem_t)(g * (__builtin_amdgcn_exp2f((list.z[j] - m) * c) / all - p));
+    if (first) out[id] = (elem_t)(g * (total * __builtin_amdgcn_exp2f((list.z[j] - m) * c) / all - p));
   }
 }
 
