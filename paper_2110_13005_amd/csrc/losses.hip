@@ -50,15 +50,17 @@ __device__ __forceinline__ float block_all(float v, float (&shared)[THREADS / 64
 
 // exp((z - m) / temperature) as exp2(z c - m c) with c = log2(e) / temperature: one fused multiply-add and one exponential.  m c is
 // rounded; every exponential of the row is off by the same factor 2^low, which cancels in the softmax and is taken out of the
-// logarithm of their sum.  Where m c comes near the largest number (a bfloat16 row whose maximum is about the type's largest or, with
-// nothing else in it, lowest value) other values than m lie so far below it that any c gives them 0: a power of two, with which
-// that of m is exact.
+// logarithm of their sum.  |low| is |m c| 2^-24 at most: 2^low would leave 32 bits' range for a row whose maximum is a mask's value, or at a
+// very low temperature.  From |m c| = 2^24 on any other 16-bit value lies 2^-11 |m| or more below m (bfloat16: 2^-8) and has the exponential 0
+// whatever c of about that size it is formed with: the power of two below c, with which m c is exact; 2^-30 where even that comes near the
+// largest number.
 struct Exponent {
   float c, m, mc, low;
   // from the maximum m, the same in all lanes; of nothing but -inf (or NaN, which has to stay) from 0
   __device__ __forceinline__ Exponent(float m_, float c_) {
     m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m_ == -INFINITY ? 0.f : m_)));
-    c = fabsf(m) * c_ < 0x1p126f ? c_ : 0x1p-30f;
+    const float size = fabsf(m) * c_;
+    c = size < 0x1p24f ? c_ : size < 0x1p126f ? __uint_as_float(__float_as_uint(c_) & 0x7f800000u) : 0x1p-30f;
     mc = m * c;
     low = m == INFINITY ? 0.f : fmaf(m, c, -mc);
   }
@@ -532,7 +534,8 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
   if (a.teacher_lse) {
     rest = r_sum == 0.f ? 0.f : 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;
-    if (rest != 0.f) loss += rest * (logf(rest) - ((r.e.m - m) * per + logf(r_sum) - log_all));
+    // (the logits' distance, which may be a mask's, times all its factors at once)
+    if (rest != 0.f) loss += rest * (logf(rest) - (logf(r_sum) - log_all)) - (r.e.m - m) * (rest * per);
     else total = list.mass;
   }
   if (tid == 0) a.token_loss[t] = loss;

@@ -1,0 +1,96 @@
+"""GPU parity of the losses over logits with their float64 definitions where logits lie far from 0: masks by large finite values, rows
+that are one such value, rows with an offset.  A log-sum-exp is then known to its own rounding only, or the product of a logit and the
+exponent's factor is; the softmax of the row is as well known as any.
+
+Bounds: fp32 arithmetic is off by U = 2^-24 of the magnitudes that go into it, counted along the formulas; a 16-bit result is rounded once
+more (`within`)."""
+import numpy as np
+import pytest
+
+from oracle import packed_ops as P
+from paper_2110_13005_amd import binding as B
+from paper_2110_13005_amd.inputs import snap_elem
+from helpers import dev_i32, host
+from test_gpu_distillation import Distillation, student
+from test_gpu_losses import empty, f32
+from test_gpu_step_ops import Padded, U, within
+
+pytestmark = [pytest.mark.gpu, pytest.mark.parametrize("axonn_elem", ["bf16", "fp16"], indirect=True)]
+VOCABULARIES = [2100, 12289, 40000, 140001]          # 256, 512 and 1024 threads a row, and more columns than registers hold
+
+
+def far_values():
+    """Masks of this type: the largest is the type's lowest value."""
+    lowest = {"bf16": -float(2 - 2 ** -7) * 2.0 ** 127, "fp16": -65504.0}[B.ELEM]
+    return [float(v) for v in snap_elem(np.array({"bf16": [-1e4, -1e6, -1e8, -1e9, -1e10, -1e15, -1e30], "fp16": [-1e4, -3e4]}[B.ELEM], np.float32))] + [lowest]
+
+
+def softmax_bounds(z):
+    """Of a row's log-sum-exp counted from its maximum, and of every element of its softmax, relative."""
+    z = np.asarray(z, np.float64)
+    V = z.shape[1]
+    gap = np.where(np.isfinite(z), z.max(axis=1, keepdims=True) - z, 0.0)
+    row = U * (60 + V / 512 + 4 * np.sum(np.exp(P.log_softmax(z)) * gap, axis=1) + 4 * np.log(V + 1))
+    return row, row[:, None] + U * (8 + 6 * np.minimum(gap, 1e4))
+
+
+@pytest.mark.parametrize("mass", [None, 0.7, 1.0])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0, 8.0, 2.0 ** -12, 2.0 ** 14])
+def test_distillation_with_all_but_the_named_masked(tau, mass):
+    T, V, K = 3, 2100, 40
+    for i, value in enumerate(far_values()):
+        rng = np.random.default_rng(i)
+        ids = np.argsort(rng.random((T, V)), axis=1)[:, :K]
+        named = student(rng, T, V, ids) * min(tau, 1.0)
+        z = np.full((T, V), value, np.float32)
+        np.put_along_axis(z, ids, snap_elem(np.take_along_axis(named, ids, axis=1).astype(np.float32)), axis=1)
+        u = rng.standard_normal((T, K)) * tau
+        if mass is not None:
+            u -= tau * np.log(np.exp(u / tau).sum(axis=1, keepdims=True) / mass)
+        # a power of two: the products by 1 / temperature are exact, and so is the division
+        d = Distillation(z, u.astype(np.float32), ids, None if mass is None else np.zeros(T, np.float32), tau, np.full(T, tau if tau < 1 else 1.0, np.float32))
+        d.run()
+        d.check()
+
+
+def rows_of(value, V, lower):
+    """Half of the columns at `value`, the others below it; a row of nothing but it; one that holds it once."""
+    rng = np.random.default_rng(V)
+    z = np.full((3, V), value, np.float32)
+    z[0, rng.random(V) < 0.5] = lower
+    z[2] = lower
+    targets = np.array([int(np.flatnonzero(z[0] == value)[3]), V // 3, V - 2])
+    z[2, V - 2] = value
+    return z, targets
+
+
+@pytest.mark.parametrize("lower", ["masked", "lowest"])
+@pytest.mark.parametrize("V", VOCABULARIES)
+def test_rows_whose_maximum_is_far(V, lower):
+    for value in far_values():
+        below = -np.inf if lower == "masked" else far_values()[-1]
+        z, targets = rows_of(value, V, below)
+        T = len(z)
+        buf, grad = Padded(T, V, values=z), Padded(T, V)
+        t, ones = dev_i32(targets), f32(np.ones(T))
+        logp, lse, token = empty(T), empty(T), empty(T)
+        want, want_lse = P.token_logprobs(z, targets)
+        row, rel = softmax_bounds(z)
+        B.axonn_token_logprobs_fwd(T, V, buf.t, V, t, logp, lse)
+        assert (np.abs(host(logp) - want) <= row + 3 * U * np.abs(want)).all(), value
+        assert (np.abs(host(lse) - want_lse) <= row + 2 * U * np.abs(want_lse)).all(), value
+        # a ratio of about 1, which no limit clips
+        old = want.astype(np.float32)
+        B.axonn_policy_loss(T, V, buf.t, V, t, f32(old), None, ones, ones, 0.2, 0.2, 0.0, 1.0, logp, token, None, grad.t, V)
+        _, r_token, _, r_d = P.policy_loss(z, targets, old, None, np.ones(T), np.ones(T), 0.2, 0.2, 0.0)
+        e = 2 * row + U * (16 + 8 * np.abs(want))
+        assert (np.abs(host(logp) - want) <= row + 3 * U * np.abs(want)).all(), value
+        assert (np.abs(host(token) - r_token) <= 2 * e).all(), value
+        q, onehot = np.exp(P.log_softmax(z)), np.arange(V) == targets[:, None]
+        within(grad.result(), r_d, q * rel + 4 * e[:, None] * (q + onehot), label=("policy", value))
+        # a teacher that names the target and another one
+        ids = np.stack([targets, (targets + 7) % V], axis=1)
+        z[np.arange(T), ids[:, 1]] = value
+        d = Distillation(z, np.zeros((T, 2), np.float32), ids, np.full(T, 1.0, np.float32), 1.0, np.ones(T, np.float32))
+        d.run()
+        d.check()
