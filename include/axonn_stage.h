@@ -631,7 +631,9 @@ int axonn_attention_packed_bwd(int64_t T, int32_t n_seq, int32_t n_heads, int32_
 int axonn_token_logprobs_fwd(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_logits,
                              const int32_t* targets, float* logp, float* lse, void* hip_stream);
 /* Its gradient: dlogits = dlogp[t] (onehot(target) - softmax(z)); rows of zeros for tokens without a
- * target and where dlogp[t] is 0.  dlogits may be logits. */
+ * target and where dlogp[t] is 0.  dlogits may be logits.  lse: what the forward pass has left; the softmax
+ * is exp(z - lse) where |lse| < 2^10, whose rounding moves it by less than 2^-13 of itself, and formed
+ * from the row anew where it is farther from 0 (slower). */
 int axonn_token_logprobs_bwd(int64_t T, int64_t V, const void* logits_bf16, int64_t ld_logits,
                              const int32_t* targets, const float* lse, const float* dlogp,
                              void* dlogits_bf16, int64_t ld_dlogits, void* hip_stream);

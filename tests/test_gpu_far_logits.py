@@ -94,3 +94,29 @@ def test_rows_whose_maximum_is_far(V, lower):
         d = Distillation(z, np.zeros((T, 2), np.float32), ids, np.full(T, 1.0, np.float32), 1.0, np.ones(T, np.float32))
         d.run()
         d.check()
+
+
+@pytest.mark.parametrize("V", VOCABULARIES)
+def test_gradient_of_rows_with_an_offset(V):
+    """The softmax of a row does not change with an offset, although its log-sum-exp is rounded ever more coarsely; in place too."""
+    rng = np.random.default_rng(V)
+    offsets = np.array([0.0, 900.0, -900.0, 1500.0, -3000.0, 20000.0, -20000.0] + far_values())
+    T = len(offsets) + 3
+    z = snap_elem((np.maximum(np.append(offsets, [0, 5000.0, 5000.0])[:, None] + 2 * rng.standard_normal((T, V)), far_values()[-1])).astype(np.float32))
+    z = np.asarray(z, np.float32).reshape(T, V)
+    targets = rng.integers(0, V, T)
+    targets[:-3] = z[:-3].argmax(axis=1)
+    d = rng.standard_normal(T).astype(np.float32)
+    targets[-2], d[-1] = -100, 0.0
+    buf, grad, t = Padded(T, V, V + 3, 1, z), Padded(T, V, V + 5, 3), dev_i32(targets)
+    logp, lse = empty(T), empty(T)
+    B.axonn_token_logprobs_fwd(T, V, buf.t, V + 3, t, logp, lse)
+    B.axonn_token_logprobs_bwd(T, V, buf.t, V + 3, t, lse, f32(d), grad.t, V + 5)
+    row, rel = softmax_bounds(z)
+    q, slope = np.exp(P.log_softmax(z)), np.where(P.has_target(targets, V), np.abs(d), 0.0)[:, None]
+    # up to 2^10 the softmax goes by the rounded log-sum-exp
+    rel = rel + row[:, None] + 4 * U * np.minimum(np.abs(P.token_logprobs(z, np.abs(targets))[1]), 1024.0)[:, None]
+    within(grad.result(), P.token_logprobs_bwd(z, targets, d), slope * (q * rel + 4 * U * (q + (np.arange(V) == targets[:, None]))))
+    assert not grad.result()[-2:].any()
+    B.axonn_token_logprobs_bwd(T, V, buf.t, V + 3, t, lse, f32(d), buf.t, V + 3)
+    assert (buf.result() == grad.result()).all()
