@@ -549,11 +549,12 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
   const RowStats r = row.stats(c, shared);
   const float r_sum = r.sum * __builtin_amdgcn_exp2f(-r.e.low);
   const float m = list.sum == 0.f ? r.e.m : r_sum > 0.f ? fmaxf(list.top, r.e.m) : list.top;
-  const float others = __builtin_amdgcn_exp2f((r.e.m - m) * c), all = list.sum * __builtin_amdgcn_exp2f((list.top - m) * c) + (r_sum > 0.f ? r_sum * others : r_sum);
+  const float top = list.sum == 0.f ? m : list.top;   // (of named tokens that are all masked there is none)
+  const float others = __builtin_amdgcn_exp2f((r.e.m - m) * c), all = list.sum * __builtin_amdgcn_exp2f((top - m) * c) + (r_sum > 0.f ? r_sum * others : r_sum);
   const float log_all = logf(all);
   // The others' mass is an outcome of its own, if it has one and the student has other tokens (if not, what 1 - mass is may be its rounding,
   // which would count infinitely); total: the mass of all outcomes, 1 with that one.
-  float loss = list.gain + list.mass * ((m - list.top) * per + log_all), rest = 0.f, total = 1.f;
+  float loss = list.gain + list.mass * ((m - top) * per + log_all), rest = 0.f, total = 1.f;
   if (a.teacher_lse) {
     rest = r_sum == 0.f ? 0.f : 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;

@@ -120,3 +120,29 @@ def test_gradient_of_rows_with_an_offset(V):
     assert not grad.result()[-2:].any()
     B.axonn_token_logprobs_bwd(T, V, buf.t, V + 3, t, lse, f32(d), buf.t, V + 3)
     assert (buf.result() == grad.result()).all()
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0])
+@pytest.mark.parametrize("lse", [None, 3.0])
+def test_distillation_of_named_tokens_without_probability(lse, tau):
+    """The student masks all that the teacher names: the loss is infinite, its gradient is not; wherever the others' logits lie."""
+    T, V, K = 5, 2100, 3
+    rng = np.random.default_rng(1)
+    z = np.asarray(normal_at([0.0, -30.0, -100.0, -3000.0, 60.0], rng, V), np.float32)
+    ids = np.argsort(rng.random((T, V)), axis=1)[:, :K]
+    np.put_along_axis(z, ids, -np.inf, axis=1)
+    d = Distillation(z, np.zeros((T, K), np.float32), ids, None if lse is None else np.full(T, lse, np.float32), tau, np.ones(T, np.float32))
+    d.run()
+    with np.errstate(all="ignore"):
+        token, _, dz = P.distill_loss(z, d.u, ids, d.lse, tau, d.w)
+    assert (token == np.inf).all() and (host(d.token) == np.inf).all()
+    row, rel = softmax_bounds(z / tau)
+    q, p = np.exp(P.log_softmax(z / tau)), np.zeros((T, V))
+    np.put_along_axis(p, ids, 1 / 3 if lse is None else np.exp(-lse), axis=1)
+    rest = 1 - p.sum(axis=1, keepdims=True)
+    # of the others: q (1 - rest / Q), Q = 1: of both parts and of the rest's mass
+    within(d.grad.result() / d.scale, dz, (q * (rel + row[:, None]) * (1 + rest) + 32 * U * (q + p)) / tau)
+
+
+def normal_at(offsets, rng, V):
+    return snap_elem((np.array(offsets)[:, None] + rng.standard_normal((len(offsets), V))).astype(np.float32)).reshape(len(offsets), V)
