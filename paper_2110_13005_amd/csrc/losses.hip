@@ -497,7 +497,8 @@ __device__ __forceinline__ void distill_list(const DistillArgs& a, int64_t t, co
     const float z = l.z[j], logp = l.p[j] - lse_u, p = expf(logp);
     l.p[j] = p;
     mass += p;
-    if (p != 0.f) gain += p * (logp - (z - from) * per);
+    // (a logit's distance, which may be a mask's, times all its factors at once)
+    if (p != 0.f) gain += p * logp - (z == -INFINITY ? -INFINITY : (z - from) * (p * per));
     bool first = true;
     if (twice)
       for (int i = 0; i < j; ++i) first &= l.id[i] != id;
@@ -554,11 +555,10 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
   const float log_all = logf(all);
   // The others' mass is an outcome of its own, if it has one and the student has other tokens (if not, what 1 - mass is may be its rounding,
   // which would count infinitely); total: the mass of all outcomes, 1 with that one.
-  float loss = list.gain + list.mass * ((m - top) * per + log_all), rest = 0.f, total = 1.f;
+  float loss = list.gain + ((m - top) * (list.mass * per) + list.mass * log_all), rest = 0.f, total = 1.f;
   if (a.teacher_lse) {
     rest = r_sum == 0.f ? 0.f : 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;
-    // (the logits' distance, which may be a mask's, times all its factors at once)
     if (rest != 0.f) loss += rest * (logf(rest) - (logf(r_sum) - log_all)) - (r.e.m - m) * (rest * per);
     else total = list.mass;
   }

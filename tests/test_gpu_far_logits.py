@@ -146,3 +146,37 @@ def test_distillation_of_named_tokens_without_probability(lse, tau):
 
 def normal_at(offsets, rng, V):
     return snap_elem((np.array(offsets)[:, None] + rng.standard_normal((len(offsets), V))).astype(np.float32)).reshape(len(offsets), V)
+
+
+@pytest.mark.parametrize("tau", [0.25, 1.0])
+def test_distillation_of_entries_without_mass(tau):
+    """The teacher gives what it names no mass, and the student masks it by its type's lowest value: all that counts are the others."""
+    T, V, K = 4, 2100, 3
+    rng = np.random.default_rng(2)
+    z = np.asarray(normal_at([0.0, 3.0, -40.0, 40.0], rng, V), np.float32)
+    ids = np.argsort(rng.random((T, V)), axis=1)[:, :K]
+    np.put_along_axis(z, ids, far_values()[-1], axis=1)
+    d = Distillation(z, np.full((T, K), -500.0 * tau, np.float32), ids, np.zeros(T, np.float32), tau, np.ones(T, np.float32))
+    d.run()
+    scaled = z.astype(np.float64) / tau
+    row, rel = softmax_bounds(scaled)
+    # all mass is the others', of both: log 1 - log 1, and no gradient
+    assert (np.abs(host(d.token)) <= 2 * row + 8 * U).all()
+    q = np.exp(P.log_softmax(scaled))
+    within(d.grad.result() / d.scale, np.zeros((T, V)), (2 * q * (rel + row[:, None]) + 8 * U * q) / tau)
+
+
+@pytest.mark.parametrize("tau", [0.25, 1.0])
+@pytest.mark.parametrize("lse", [None, 0.5])
+def test_distillation_of_a_masked_entry_of_little_mass(lse, tau):
+    """The student masks one of the teacher's entries by its type's lowest value: its mass times the distance counts, however far that is."""
+    T, V, K = 4, 2100, 3
+    rng = np.random.default_rng(3)
+    z = np.asarray(normal_at([0.0, 3.0, -40.0, 40.0], rng, V), np.float32)
+    ids = np.argsort(rng.random((T, V)), axis=1)[:, :K]
+    z[np.arange(T), ids[:, 1]] = far_values()[-1]
+    u = np.tile(np.array([0.0, -20.0, -1.0]) * tau, (T, 1)).astype(np.float32)
+    d = Distillation(z, u, ids, None if lse is None else np.full(T, lse, np.float32), tau, np.ones(T, np.float32))
+    d.run()
+    d.check()
+    assert np.isfinite(host(d.token)).all()
