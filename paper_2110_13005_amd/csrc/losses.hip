@@ -306,18 +306,19 @@ __global__ __launch_bounds__(GRAD_THREADS) void token_logprobs_bwd_kernel(int V,
   constexpr int COLUMNS = 8 * GRAD_THREADS * CHUNKS;
   const uint32_t t = host::recip_div(blockIdx.x, parts, parts_recip), first = (blockIdx.x - t * parts) * COLUMNS;
   const int target = targets[t], tid = threadIdx.x, n = min(V - (int)first, COLUMNS);
-  const float slope = target < 0 || target >= V ? 0.f : dlogp[t], lse_t = lse[t];
+  const float slope = target < 0 || target >= V ? 0.f : dlogp[t];
   elem_t* const out = dlogits + t * ld_d + first;
   if (slope == 0.f) {
     store_zeros<GRAD_THREADS>(out, n, tid);
     return;
   }
+  Row<GRAD_THREADS, CHUNKS, 0> row;
+  row.load(logits + t * ld + first, n, tid);
+  const float lse_t = lse[t];                         // on its way beside the row
   if (fabsf(lse_t) >= FAR_LSE) {
     if (first == 0) far_row_gradient(V, logits + t * ld, target, slope, out, tid);
     return;
   }
-  Row<GRAD_THREADS, CHUNKS, 0> row;
-  row.load(logits + t * ld + first, n, tid);
   const Exponent e(lse_t, kLog2eLoss);
   const bool here = target >= (int)first && target < (int)first + n;
   const float at_target = here ? (float)logits[t * ld + target] : 0.f;
