@@ -280,7 +280,7 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void token_logprobs_fwd
 // us (6.5 TB/s, the caches still hold a part of the logits).
 constexpr int GRAD_THREADS = 256;
 // From here on a rounded log-sum-exp does not say what the softmax is: half a step of it is 2^-14 and more.  The row's first workgroup forms
-// both from the logits, alone, so that it may be in place: 2758 x 51200 of such rows 189 us, 104 with lse (all tokens with a target).
+// both from the logits, alone, so that it may be in place: 2758 x 51200 of such rows 212 us, 100 with lse (all tokens with a target).
 constexpr float FAR_LSE = 1024.f;
 __device__ __forceinline__ void far_row_gradient(int V, const elem_t* row, int target, float slope, elem_t* out, int tid) {
   __shared__ RowShared<GRAD_THREADS> shared;
@@ -447,6 +447,10 @@ struct DistillList {
   float top, sum;                          // of the named tokens' logits, each once: maximum; sum of exp((z - top) / temperature)
   float gain;                              // sum of p (log p - (z - top) / temperature)
 };
+// sum + w (distance * per + more), w_per = w * per: a mask's distance may pass the largest number with its factor, but not with both.
+__device__ __forceinline__ float add_weighted(float sum, float w, float w_per, float distance, float more) {
+  return fmaf(distance, w_per, fmaf(w, more, sum));
+}
 // id, u: the lane's first entry, if it has one
 __device__ __forceinline__ void distill_list(const DistillArgs& a, int64_t t, const elem_t* row, uint32_t* named, DistillList& l, int lane, int id,
                                              float u, int& twice) {
@@ -498,8 +502,8 @@ __device__ __forceinline__ void distill_list(const DistillArgs& a, int64_t t, co
     const float z = l.z[j], logp = l.p[j] - lse_u, p = expf(logp);
     l.p[j] = p;
     mass += p;
-    // (a logit's distance, which may be a mask's, times all its factors at once)
-    if (p != 0.f) gain += p * logp - (z == -INFINITY ? -INFINITY : (z - from) * (p * per));
+    const float p_per = p * per;
+    if (p_per != 0.f) gain = add_weighted(gain, p, p_per, from - z, logp);
     bool first = true;
     if (twice)
       for (int i = 0; i < j; ++i) first &= l.id[i] != id;
@@ -556,11 +560,11 @@ __global__ __launch_bounds__(THREADS, row_waves(CHUNKS)) void distill_loss_kerne
   const float log_all = logf(all);
   // The others' mass is an outcome of its own, if it has one and the student has other tokens (if not, what 1 - mass is may be its rounding,
   // which would count infinitely); total: the mass of all outcomes, 1 with that one.
-  float loss = list.gain + ((m - top) * (list.mass * per) + list.mass * log_all), rest = 0.f, total = 1.f;
+  float loss = add_weighted(list.gain, list.mass, list.mass * per, m - top, log_all), rest = 0.f, total = 1.f;
   if (a.teacher_lse) {
     rest = r_sum == 0.f ? 0.f : 1.f - list.mass;
     if (rest < 0.f) rest = 0.f;
-    if (rest != 0.f) loss += rest * (logf(rest) - (logf(r_sum) - log_all)) - (r.e.m - m) * (rest * per);
+    if (rest != 0.f) loss = add_weighted(loss, rest, rest * per, m - r.e.m, logf(rest) - (logf(r_sum) - log_all));
     else total = list.mass;
   }
   if (tid == 0) a.token_loss[t] = loss;
