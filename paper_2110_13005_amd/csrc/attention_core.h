@@ -745,7 +745,8 @@ __device__ __forceinline__ void attn_bwd_dkdv(DkdvLds<D>& lds, int kt, int s, in
 // when they do not run with others.  FORM_DELTA_ANY: for any d, in an order of its own.
 // PINNED: the accumulators in the accumulation registers, scores and all operands in ordinary ones, by assembly (see mfma32_agpr); for
 // a wave that is alone on its SIMD.  The compiler, which gives every MFMA of such a kernel accumulation registers, otherwise moves values
-// between the two kinds for a sixth of what the loop issues.  Backward of 2 x 36 heads of 176 x 2048 489 -> 477 us.
+// between the two kinds for a sixth of what the loop issues.  Backward of 2 x 36 heads of 176 x 2048, in turn
+// on one machine, 489 -> 477 us (on another one 457).
 //
 // Two workgroups share a CU.  The fragments run a few MFMAs ahead through a ring, so that a wave waits for LDS only behind the
 // two barriers of a tile: one when everybody has left the tile before, whose buffer the memory pipeline then fills, one when

@@ -506,16 +506,19 @@ inline int choose_fp8_tile(int64_t M, int64_t N, int64_t nk, bool fp32_result) {
 
 // ---------------------------------------------------------------------- backward pass of attention over packed sequences
 // dQ and dK / dV as one launch?  Above 128 columns a workgroup of either kind has a CU to itself, and one grid has one tail instead of
-// two: 2 x 36 heads of 176 x 2048 528 -> 459 us, 24 heads of 188, seven sequences of about 512, 159 -> 130.  Below, the dQ workgroups
+// two, in turn on one machine and with dQ's accumulators where the compiler put them: 2 x 36 heads of 176 x 2048 528 -> 459 us, 24 heads of
+// 188, seven sequences of about 512, 159 -> 130 (pinned, on another one, 457 and 126).  Below, the dQ workgroups
 // share a CU on their own but not beside the others: one launch while both kinds find a CU each (tiles x heads).  Four sequences of 256, 8
 // heads of 128 24.6 -> 15.6; 12 of 300, 16 heads of 64 (576 tiles) 31.9 in two launches, 33.1 in one.
 inline bool packed_one_launch(int64_t tiles_heads, int columns) { return columns > 128 || tiles_heads <= 256; }
 
 // Workgroups that share a tile of keys in the dK / dV kernel, each with an equal part of the group's heads; above 1 a launch behind it
 // adds their sums up.  The least modelled time, us: the longest chain of query tiles or the work of all tiles over 256 CUs, whichever
-// is longer, and the joining launch with what is written and read for it.  The host knows the sequences' number alone: equal lengths.
+// is longer, and the joining launch with what is written and read for it.  The host knows the sequences' number alone and takes them as equally
+// long: one long among many short or empty ones is one long chain in too few parts (7000 of 8192 rows, 16 heads on 2 of 128: among 20 others 870
+// us, among 255 1453; one sequence of 8192 832).
 // Measured (modelled choice in brackets): one sequence of 8192, 16 heads on 4 of 128, 1 part 1072, [2] 861, 4 870; 31 of 90 to 1, 16 on 2
-// of 64, 1 28, [4] 20, 8 23; 2048, 32 on 1 of 128, 1 1357, [32] 165; six of 600, 32 on 8 of 160 [1] 149, 2 174; 16 of 512, 16 on 4 of 64 [1] 62, 2 66.
+// of 64, 1 28, [4] 20, 8 23; 2048, 32 on 1 of 128, 1 1357, [32] 146; six of 600, 32 on 8 of 160 [1] 149, 2 174; 16 of 512, 16 on 4 of 64 [1] 62, 2 66.
 constexpr int64_t kMaxParts = 4096;      // of all tiles together: at most 800 MB of partial sums
 inline int packed_parts(int64_t T, int64_t n_seq, int heads, int kv, int columns) {
   const int group = heads / kv;
